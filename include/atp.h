@@ -533,6 +533,150 @@ int atp_kv_evict_lru(const int32_t *table, int32_t n_seq, int32_t max_blocks, in
                      const int64_t *last_use, uint64_t block_bytes, uint64_t budget_bytes,
                      int32_t compact, int32_t *keep, int32_t *new_table, atp_evict_stats *stats);
 
+/* ---- KV cache operators of a serving step (Sec. III-B: KV-cache operators
+ * with variable-length shards) ---------------------------------------------
+ * What a rank does to its paged cache between two reshards, on head ranges
+ * of unequal width (a range may begin and end inside a GQA group):
+ *   atp_kv_extend  blocks, slots and positions for the new tokens, from the
+ *                  block table and the request lengths
+ *   atp_kv_append  rotary positions on q and k; k and v into their slots
+ *   atp_kv_attend  attention of the new tokens over the cache: one token per
+ *                  sequence, a few, or whole prompts (the replay of sessions
+ *                  that atp_kv_evict_lru dropped)
+ * They run on the arena and the block table that atp_reshard_kv leaves.
+ * Each call checks its arguments before the first HIP call, then enqueues
+ * kernels on `stream` (a stream of the current device, else ATP_EINVAL) and
+ * returns; none allocates, waits or copies to the host, so all of them may
+ * be captured into a HIP graph.  Workspaces need no initial value and hold
+ * nothing from one call to the next; calls that may run at once need
+ * workspaces of their own.  Lengths are read on the device: the host gives
+ * only bounds (max_*), so a captured step replays with other lengths. */
+enum { ATP_BF16 = 0, ATP_FP16 = 1, ATP_E4M3 = 2 }; /* E4M3: OCP, 448 max, NaN, no infinity */
+
+/* The cache of one rank, as the operators see it: the arena of atp_kv with
+ * its element types and this rank's heads. */
+typedef struct {
+  void *arena;             /* device, 256-byte aligned; atp_kv_extend: unused */
+  uint64_t arena_bytes;
+  int32_t num_layers, block_tokens, head_dim, layout; /* as in atp_kv; head_dim a multiple of 8, at most 256 */
+  int64_t num_blocks;
+  atp_range q_heads, kv_heads; /* this rank's ranges, as atp_plan_ranges reports them:  */
+  int32_t group;               /* query head h reads KV head h / group; every KV head
+                                  that q_heads needs must lie in kv_heads (else EINVAL) */
+  int32_t dtype;               /* of q, k, v and the outputs: ATP_BF16 or ATP_FP16       */
+  int32_t cache_dtype;         /* of the arena: the same, or ATP_E4M3                    */
+  int32_t reserved;
+  const float *scales; /* E4M3: device float [num_layers][2][KV heads], positive: an
+                          element stands for its value times its scale; else NULL */
+} atp_kv_cache;
+
+/* One step's requests.  Rows of q, k, v and the outputs are tokens, sequence
+ * by sequence: those of sequence s are [starts[s], starts[s + 1]).  Rows from
+ * starts[n_seq] to max_tokens are padding: outputs are left as they were. */
+typedef struct {
+  int32_t *block_table;  /* device [n_seq][max_blocks], -1 = unused          */
+  int32_t n_seq, max_blocks;
+  const int32_t *cached; /* device [n_seq]: tokens in the cache before       */
+  const int32_t *fresh;  /* device [n_seq]: tokens the step adds (0 or more) */
+  int32_t *starts;       /* device [n_seq + 1]                               */
+  int64_t *slots;        /* device [max_tokens]: block * block_tokens +
+                            offset of each token, -1 = padding               */
+  int32_t *positions;    /* device [max_tokens]: position in its sequence    */
+  int32_t max_tokens;    /* rows                                             */
+  int32_t max_fresh;     /* at least every fresh[s]           (atp_kv_attend) */
+  int32_t max_ctx;       /* at least every cached[s] + fresh[s]      (same)   */
+  int32_t reserved;
+  int32_t *status;       /* device [4]: status code of the step (0 = ATP_OK),
+                            tokens, blocks taken, blocks still free.
+                            atp_kv_extend writes all four; append and attend
+                            set the code on a bad slot or block id and never
+                            clear it (they take NULL: nothing is reported)    */
+} atp_kv_step;
+
+/* Give the new tokens of every sequence their places.  `table` (device
+ * [n_seq][max_blocks], read only unless it is step->block_table) plus new
+ * blocks becomes step->block_table: of sequence s, the blocks that hold its
+ * tokens [cached, cached + fresh) and are -1 in `table` take the ids that no
+ * entry of `table` names, ascending, in (sequence, block) order; every other
+ * entry is kept.  Writes starts (exclusive sums of fresh), slots and
+ * positions (-1 and 0 behind the last token) and status.
+ * The step is all or nothing.  When a length is negative, a sequence would
+ * pass max_blocks, the tokens pass max_tokens, an id lies outside
+ * [-1, num_blocks), or a block that takes new tokens is named by another
+ * entry too (a shared block: copy it first), status[0] is ATP_EINVAL; when
+ * too few blocks are free, ATP_ECAPACITY.  block_table then equals `table`,
+ * starts is all 0 and slots all -1, so that append and attend do nothing;
+ * status[1..3] are 0 tokens, the blocks that were wanted and the free ones
+ * (both 0 after ATP_EINVAL).
+ * Uses cache->block_tokens and num_blocks alone, and every field of the step
+ * but max_fresh and max_ctx. */
+int atp_kv_extend_workspace(const atp_kv_cache *cache, const atp_kv_step *step, uint64_t *bytes);
+int atp_kv_extend(const atp_kv_cache *cache, const atp_kv_step *step, const int32_t *table,
+                  void *workspace, uint64_t workspace_bytes, atp_stream stream);
+
+/* Rotary positions: pair i of the first rot_dim dimensions (rot_dim / 2
+ * pairs: dimensions (i, i + rot_dim / 2), or (2i, 2i + 1) with
+ * `interleaved`) turns by position * f_i, f_i = base^(-2i / rot_dim); the
+ * rest of the head is kept.  Scaling for long contexts:
+ *   LINEAR  f_i / factor
+ *   PARTS   by the turns r_i = original * f_i / (2 pi) that a pair makes over
+ *           the original context: f_i where r_i > high, f_i / factor where
+ *           r_i < low, and linear in r_i between them
+ * amplitude multiplies the cosine and the sine (1 for none).  Angles are
+ * reduced in 64 bits: positions up to 2^31 keep their phase. */
+enum { ATP_ROPE_PLAIN = 0, ATP_ROPE_LINEAR = 1, ATP_ROPE_PARTS = 2 };
+typedef struct {
+  int32_t rot_dim; /* even, 0 (no rotation) .. head_dim */
+  int32_t interleaved;
+  int32_t scaling;
+  int32_t reserved;
+  double base, factor, low, high, original, amplitude;
+} atp_rope;
+
+/* Rotate q and k (rope NULL: no rotation) and write k and v of `layer` into
+ * the cache at step->slots.  q: [max_tokens][query heads][head_dim] with
+ * q_stride elements from token to token; k and v likewise with the KV heads;
+ * q_out as q (may be q itself with the same stride, else it must not overlap
+ * the inputs).  Rows are 16-byte aligned: pointers and strides (ATP_EALIGN).
+ * The arithmetic is in 32 bits and rounded once; to E4M3, k and v are divided
+ * by their scale and values beyond 448 become 448.  A token whose slot is
+ * negative is padding: nothing of it is read or written.  Slots must differ
+ * from each other.  A slot past the arena sets status and is skipped (its q
+ * is still rotated).  Uses slots, positions, max_tokens and status. */
+int atp_kv_append(const atp_kv_cache *cache, const atp_kv_step *step, int32_t layer, const atp_rope *rope,
+                  const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                  void *q_out, int64_t q_out_stride, atp_stream stream);
+
+/* What a token of the step sees: of its own sequence the tokens t at or
+ * before its position p, with `window` > 0 only those with p - t < window,
+ * and none whose block is -1 in the table.  The score of query head h is
+ * scale * q.k, then softcap * tanh(score / softcap) if softcap > 0, then
+ * + slopes[h] * (t - p) if slopes is given (device float [query heads]). */
+typedef struct {
+  float scale, softcap;
+  int32_t window;
+  int32_t reserved;
+  const float *slopes;
+} atp_kv_mask;
+
+/* Attention of the step's tokens over the cache of `layer`, which holds
+ * their own k and v already (atp_kv_append).  q and out as in atp_kv_append
+ * (out must not overlap q); lse (NULL, or float [max_tokens][query heads])
+ * receives the natural logarithm of the sum of exp(score).  A row that sees
+ * nothing gives 0 and -infinity.  Values in unseen places, NaN among them, do
+ * not matter.  Scores, softmax and sums are held in 32 bits; with many rows
+ * per KV head the softmax weights enter the second product rounded to dtype.
+ * A block id outside [-1, num_blocks) sets status and counts as -1.  A
+ * sequence whose starts, cached or lengths break a bound (max_tokens,
+ * max_fresh, max_ctx, max_blocks) sets status and its rows are left as they
+ * were.  The result of a call depends on its inputs and bounds alone (sums
+ * are taken in a fixed order).  Uses block_table, cached, starts, max_* and
+ * status; the workspace size depends on the bounds. */
+int atp_kv_attend_workspace(const atp_kv_cache *cache, const atp_kv_step *step, uint64_t *bytes);
+int atp_kv_attend(const atp_kv_cache *cache, const atp_kv_step *step, int32_t layer, const atp_kv_mask *mask,
+                  const void *q, int64_t q_stride, void *out, int64_t out_stride, float *lse,
+                  void *workspace, uint64_t workspace_bytes, atp_stream stream);
+
 /* ---- state plane (Sec. III-A: a daemon, decoupled from the inference
  * process, keeps the GPU memory of the weights and the KV cache; inference
  * processes obtain handles to it over IPC and read and write it, so the

@@ -30,6 +30,8 @@ KV_COMPACT = 1 << 10
 NO_TAIL_STAGING = 1 << 11
 KEEP, P2P, RELOAD = 0, 1, 2
 SEG_INFLOW_W, SEG_OUTBOUND_W, SEG_INFLOW_KV, SEG_OUTBOUND_KV = 0, 1, 2, 3
+BF16, FP16, E4M3 = 0, 1, 2
+ROPE_PLAIN, ROPE_LINEAR, ROPE_PARTS = 0, 1, 2
 
 EXPORTS = [
     "atp_plan", "atp_plan_free", "atp_reshard_weights", "atp_reshard_kv", "atp_sync",
@@ -40,6 +42,7 @@ EXPORTS = [
     "atp_state_alloc", "atp_state_open", "atp_state_release", "atp_state_free", "atp_state_put",
     "atp_state_get", "atp_state_list", "atp_state_shutdown", "atp_warmup", "atp_load_reshard_weights",
     "atp_reshard_kv_noalloc", "atp_scratch_bytes", "atp_load_reshard_weights_async", "atp_plan_load_stats",
+    "atp_kv_extend_workspace", "atp_kv_extend", "atp_kv_append", "atp_kv_attend_workspace", "atp_kv_attend",
 ]
 
 
@@ -124,6 +127,33 @@ class LoadStats(C.Structure):
                 ("tensor_bytes", C.c_uint64), ("threads", C.c_int32)]
 
 
+class KVCacheDesc(C.Structure):
+    _fields_ = [("arena", C.c_void_p), ("arena_bytes", C.c_uint64), ("num_layers", C.c_int32),
+                ("block_tokens", C.c_int32), ("head_dim", C.c_int32), ("layout", C.c_int32),
+                ("num_blocks", C.c_int64), ("q_heads", Range), ("kv_heads", Range), ("group", C.c_int32),
+                ("dtype", C.c_int32), ("cache_dtype", C.c_int32), ("reserved", C.c_int32),
+                ("scales", C.c_void_p)]
+
+
+class KVStepDesc(C.Structure):
+    _fields_ = [("block_table", C.c_void_p), ("n_seq", C.c_int32), ("max_blocks", C.c_int32),
+                ("cached", C.c_void_p), ("fresh", C.c_void_p), ("starts", C.c_void_p),
+                ("slots", C.c_void_p), ("positions", C.c_void_p), ("max_tokens", C.c_int32),
+                ("max_fresh", C.c_int32), ("max_ctx", C.c_int32), ("reserved", C.c_int32),
+                ("status", C.c_void_p)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scaling", C.c_int32),
+                ("reserved", C.c_int32), ("base", C.c_double), ("factor", C.c_double), ("low", C.c_double),
+                ("high", C.c_double), ("original", C.c_double), ("amplitude", C.c_double)]
+
+
+class MaskDesc(C.Structure):
+    _fields_ = [("scale", C.c_float), ("softcap", C.c_float), ("window", C.c_int32),
+                ("reserved", C.c_int32), ("slopes", C.c_void_p)]
+
+
 def hip_runtimes():
     """Distinct libamdhip64 files mapped into this process."""
     try:
@@ -187,6 +217,11 @@ def _load():
     lib.atp_plan_load_stats.argtypes = [P, C.POINTER(LoadStats)]
     lib.atp_kv_evict_lru.argtypes = [P, C.c_int32, C.c_int32, C.c_int64, P, C.c_uint64, C.c_uint64, C.c_int32,
                                      P, P, C.POINTER(EvictStats)]
+    lib.atp_kv_extend_workspace.argtypes = [P, P, C.POINTER(C.c_uint64)]
+    lib.atp_kv_extend.argtypes = [P, P, P, P, C.c_uint64, P]
+    lib.atp_kv_append.argtypes = [P, P, C.c_int32, P, P, C.c_int64, P, C.c_int64, P, C.c_int64, P, C.c_int64, P]
+    lib.atp_kv_attend_workspace.argtypes = [P, P, C.POINTER(C.c_uint64)]
+    lib.atp_kv_attend.argtypes = [P, P, C.c_int32, P, P, C.c_int64, P, C.c_int64, P, P, C.c_uint64, P]
     lib.atp_daemon_serve.argtypes = [C.c_char_p, C.c_int32]
     lib.atp_state_connect.argtypes = [C.c_char_p, C.POINTER(P)]
     lib.atp_state_disconnect.argtypes = [P]
@@ -374,6 +409,82 @@ def kv_evict_lru(table, last_use, num_blocks: int, block_bytes: int, budget_byte
                                 budget_bytes, int(bool(compact)), keep.ctypes.data, out.ctypes.data,
                                 C.byref(st)))
     return keep.astype(bool), out, st
+
+
+class _Described:
+    """A C description and its address (`ref`), which the calls below pass on;
+    `d` holds the fields, which may be set between calls."""
+
+    def __init__(self, d):
+        self.d = d
+        self.ref = C.addressof(d)
+
+
+class KVCache(_Described):
+    """atp_kv_cache: one rank's paged arena, its types and its head ranges."""
+
+    def __init__(self, arena, arena_bytes, num_layers, block_tokens, head_dim, num_blocks, q_heads, kv_heads, group,
+                 dtype=BF16, cache_dtype=None, layout=KV_HEAD_MAJOR, scales=0):
+        super().__init__(KVCacheDesc(arena, arena_bytes, num_layers, block_tokens, head_dim, layout, num_blocks,
+                                     Range(*q_heads), Range(*kv_heads), group, dtype,
+                                     dtype if cache_dtype is None else cache_dtype, 0, scales))
+
+
+class KVStep(_Described):
+    """atp_kv_step: one step's requests (device addresses and bounds)."""
+
+    def __init__(self, block_table, n_seq, max_blocks, cached=0, fresh=0, starts=0, slots=0, positions=0, max_tokens=0,
+                 max_fresh=0, max_ctx=0, status=0):
+        super().__init__(KVStepDesc(block_table, n_seq, max_blocks, cached, fresh, starts, slots, positions, max_tokens,
+                                    max_fresh, max_ctx, 0, status))
+
+
+class Rope(_Described):
+    """atp_rope: rotary positions."""
+
+    def __init__(self, rot_dim, base=10000.0, interleaved=False, scaling=ROPE_PLAIN, factor=1.0, low=0.0, high=0.0,
+                 original=0.0, amplitude=1.0):
+        super().__init__(RopeDesc(rot_dim, int(bool(interleaved)), scaling, 0, base, factor, low, high, original,
+                                  amplitude))
+
+
+class Mask(_Described):
+    """atp_kv_mask: score scale, tanh cap, window and slopes (a device address)."""
+
+    def __init__(self, scale, softcap=0.0, window=0, slopes=0):
+        super().__init__(MaskDesc(scale, softcap, window, 0, slopes))
+
+
+def kv_extend_workspace(cache: KVCache, step: KVStep) -> int:
+    n = C.c_uint64()
+    _check(lib.atp_kv_extend_workspace(cache.ref, step.ref, C.byref(n)))
+    return n.value
+
+
+def kv_extend(cache: KVCache, step: KVStep, table, workspace, workspace_bytes, stream) -> None:
+    """Blocks, slots and positions for the step's new tokens (atp_kv_extend)."""
+    _check(lib.atp_kv_extend(cache.ref, step.ref, table, workspace, workspace_bytes, stream))
+
+
+def kv_append(cache: KVCache, step: KVStep, layer, rope, q, q_stride, k, k_stride, v, v_stride, q_out, q_out_stride,
+              stream) -> None:
+    """Rotated q to q_out; rotated k, and v, into the cache (atp_kv_append).
+    rope may be None.  Strides are in elements."""
+    _check(lib.atp_kv_append(cache.ref, step.ref, layer, rope.ref if rope else None, q, q_stride, k, k_stride, v,
+                             v_stride, q_out, q_out_stride, stream))
+
+
+def kv_attend_workspace(cache: KVCache, step: KVStep) -> int:
+    n = C.c_uint64()
+    _check(lib.atp_kv_attend_workspace(cache.ref, step.ref, C.byref(n)))
+    return n.value
+
+
+def kv_attend(cache: KVCache, step: KVStep, layer, mask: Mask, q, q_stride, out, out_stride, lse, workspace,
+              workspace_bytes, stream) -> None:
+    """Attention of the step's tokens over the cache (atp_kv_attend); lse may be 0."""
+    _check(lib.atp_kv_attend(cache.ref, step.ref, layer, mask.ref, q, q_stride, out, out_stride, lse, workspace,
+                             workspace_bytes, stream))
 
 
 class StFiles:

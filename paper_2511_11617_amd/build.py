@@ -19,8 +19,7 @@ SYNTH_LIB = os.path.join(ROOT, "synth", "libatp_synth.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
-# Packed fp32 instructions stay off in device code (no float math here, but
-# the flag keeps every HIP translation unit built the same way).
+# Packed fp32 instructions stay off in device code.
 DEVICE_FLAGS = ["--offload-arch=" + ARCH, "-O3", "-fPIC", "-std=c++17",
                 "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
                 "-Wall", "-Wno-unused-function"]
@@ -43,13 +42,14 @@ def build_atp(out_dir: str | None = None, lib_path: str = LIB, defines=()) -> st
     os.makedirs(out_dir, exist_ok=True)
     dflags = ["-D" + d for d in defines]
     objs = []
-    for src in ("plan.cpp", "loader.cpp", "kvbudget.cpp", "state.cpp", "capi.cpp"):
+    for src in ("plan.cpp", "loader.cpp", "kvbudget.cpp", "kvops.cpp", "state.cpp", "capi.cpp"):
         obj = os.path.join(out_dir, src + ".o")
         _run(["g++", *HOST_FLAGS, *dflags, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
-    obj = os.path.join(out_dir, "exec.hip.o")
-    _run([HIPCC, *DEVICE_FLAGS, *dflags, "-c", os.path.join(CSRC, "exec.hip"), "-o", obj])
-    objs.append(obj)
+    for src in ("exec.hip", "kvstep.hip", "attend.hip"):
+        obj = os.path.join(out_dir, src + ".o")
+        _run([HIPCC, *DEVICE_FLAGS, *dflags, "-c", os.path.join(CSRC, src), "-o", obj])
+        objs.append(obj)
     tmp = lib_path + ".tmp"
     _run([HIPCC, "--offload-arch=" + ARCH, "-shared", "-fPIC", "-pthread", *objs, "-o", tmp])
     os.replace(tmp, lib_path)

@@ -10,6 +10,7 @@
 #include "../../include/atp.h"
 #include "exec.h"
 #include "kvbudget.h"
+#include "kvops.h"
 #include "loader.h"
 #include "plan.h"
 #include "state.h"
@@ -414,6 +415,50 @@ int atp_kv_evict_lru(const int32_t *table, int32_t n_seq, int32_t max_blocks, in
   return guard([&]() -> int {
     atp::evict_lru(table, n_seq, max_blocks, num_blocks, last_use, block_bytes, budget_bytes, compact != 0, keep,
                    new_table, stats);
+    return ATP_OK;
+  });
+}
+
+int atp_kv_extend_workspace(const atp_kv_cache *cache, const atp_kv_step *step, uint64_t *bytes) {
+  return guard([&]() -> int {
+    if (!bytes) return fail(ATP_EINVAL, "bytes is NULL");
+    atp::ExtendArgs a;
+    atp::extend_args(cache, step, &a);
+    *bytes = atp::extend_workspace(a);
+    return ATP_OK;
+  });
+}
+
+int atp_kv_extend(const atp_kv_cache *cache, const atp_kv_step *step, const int32_t *table, void *workspace,
+                  uint64_t workspace_bytes, atp_stream stream) {
+  return guard([&]() -> int {
+    atp::kv_extend(cache, step, table, workspace, workspace_bytes, stream);
+    return ATP_OK;
+  });
+}
+
+int atp_kv_append(const atp_kv_cache *cache, const atp_kv_step *step, int32_t layer, const atp_rope *rope, const void *q,
+                  int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *q_out,
+                  int64_t q_out_stride, atp_stream stream) {
+  return guard([&]() -> int {
+    atp::kv_append(cache, step, layer, rope, q, q_stride, k, k_stride, v, v_stride, q_out, q_out_stride, stream);
+    return ATP_OK;
+  });
+}
+
+int atp_kv_attend_workspace(const atp_kv_cache *cache, const atp_kv_step *step, uint64_t *bytes) {
+  return guard([&]() -> int {
+    if (!bytes) return fail(ATP_EINVAL, "bytes is NULL");
+    *bytes = atp::kv_attend_workspace(cache, step);
+    return ATP_OK;
+  });
+}
+
+int atp_kv_attend(const atp_kv_cache *cache, const atp_kv_step *step, int32_t layer, const atp_kv_mask *mask,
+                  const void *q, int64_t q_stride, void *out, int64_t out_stride, float *lse, void *workspace,
+                  uint64_t workspace_bytes, atp_stream stream) {
+  return guard([&]() -> int {
+    atp::kv_attend(cache, step, layer, mask, q, q_stride, out, out_stride, lse, workspace, workspace_bytes, stream);
     return ATP_OK;
   });
 }
