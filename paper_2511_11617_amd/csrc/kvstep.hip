@@ -155,6 +155,7 @@ __global__ void __launch_bounds__(kScanThreads) k_scan(ExtendArgs a, ExtendWs w)
 
 __global__ void __launch_bounds__(kStepThreads) k_list(ExtendArgs a, ExtendWs w) {
   const int32_t taken = w.found[1], words = words_of(a.num_blocks);
+  if (taken <= 0) return;  // after a refusal, rank holds nothing
   for (int32_t i = blockIdx.x * kStepThreads + threadIdx.x; i < words; i += gridDim.x * kStepThreads) {
     int32_t r = w.rank[i];
     if (r >= taken) continue;
