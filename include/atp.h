@@ -584,7 +584,7 @@ typedef struct {
   int32_t *positions;    /* device [max_tokens]: position in its sequence    */
   int32_t max_tokens;    /* rows                                             */
   int32_t max_fresh;     /* at least every fresh[s]           (atp_kv_attend) */
-  int32_t max_ctx;       /* at least every cached[s] + fresh[s]      (same)   */
+  int32_t max_ctx;       /* at least every cached[s] + fresh[s], at most 2^30 */
   int32_t reserved;
   int32_t *status;       /* device [4]: status code of the step (0 = ATP_OK),
                             tokens, blocks taken, blocks still free.

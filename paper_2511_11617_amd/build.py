@@ -9,6 +9,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -46,10 +47,11 @@ def build_atp(out_dir: str | None = None, lib_path: str = LIB, defines=()) -> st
         obj = os.path.join(out_dir, src + ".o")
         _run(["g++", *HOST_FLAGS, *dflags, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
-    for src in ("exec.hip", "kvstep.hip", "attend.hip"):
-        obj = os.path.join(out_dir, src + ".o")
-        _run([HIPCC, *DEVICE_FLAGS, *dflags, "-c", os.path.join(CSRC, src), "-o", obj])
-        objs.append(obj)
+    hip = [(src, os.path.join(out_dir, src + ".o"))
+           for src in ("exec.hip", "kvstep.hip", "attend.hip", "attend_few.hip")]
+    with ThreadPoolExecutor(len(hip)) as pool:  # the attention kernels' many variants take a minute
+        list(pool.map(lambda x: _run([HIPCC, *DEVICE_FLAGS, *dflags, "-c", os.path.join(CSRC, x[0]), "-o", x[1]]), hip))
+    objs += [obj for _, obj in hip]
     tmp = lib_path + ".tmp"
     _run([HIPCC, "--offload-arch=" + ARCH, "-shared", "-fPIC", "-pthread", *objs, "-o", tmp])
     os.replace(tmp, lib_path)

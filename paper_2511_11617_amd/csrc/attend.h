@@ -1,0 +1,139 @@
+// attend.h — what the attention kernels share: matrix instructions and their
+// operands, a sequence's range of tokens, the score's extras and mask, and
+// the places of tokens in the paged cache.
+#pragma once
+#include "kvdev.h"
+
+namespace atp {
+
+using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
+using f32x4 = float __attribute__((ext_vector_type(4)));
+using f32x16 = float __attribute__((ext_vector_type(16)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// What depends on the 16-bit type.  The softmax weights are taken as 2^(s - m
+// + kLift) with m at most 8 below the largest score: in fp16 the lift keeps
+// weights of 2^-29 of the largest one normal, and 2^15 does not overflow.
+template <typename T>
+struct Half16;
+template <>
+struct Half16<__bf16> {
+  using v8 = bf16x8;
+  using v2 = bf16x2;
+  static constexpr float kLift = 0;
+  static constexpr uint32_t kExp = 0x7f80;  // exponent bits: all set = infinity or NaN
+  static constexpr uint32_t kFrac = 0x007f;
+  static constexpr uint32_t kOne = 0x3f80;
+  static __device__ f32x4 mfma16(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static __device__ f32x16 mfma32(v8 a, v8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static __device__ uint32_t fp8_lo(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false)); }
+  static __device__ uint32_t fp8_hi(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true)); }
+};
+template <>
+struct Half16<_Float16> {
+  using v8 = f16x8;
+  using v2 = f16x2;
+  static constexpr float kLift = 7;
+  static constexpr uint32_t kExp = 0x7c00;
+  static constexpr uint32_t kFrac = 0x03ff;
+  static constexpr uint32_t kOne = 0x3c00;
+  static __device__ f32x4 mfma16(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+  static __device__ f32x16 mfma32(v8 a, v8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+  static __device__ uint32_t fp8_lo(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, false)); }
+  static __device__ uint32_t fp8_hi(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, true)); }
+};
+
+template <typename T>
+__device__ inline uint32_t pack2(float a, float b) {
+  typename Half16<T>::v2 v = {T(a), T(b)};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// Two dwords of 16-bit pairs -> their low halves, their high halves.
+__device__ inline uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100); }
+__device__ inline uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302); }
+
+// x / d for x < 2^31 with magic = ceil(2^64 / d) (0 for d = 1).
+__device__ inline uint32_t divided(uint32_t x, uint64_t magic) { return magic ? uint32_t(__umul64hi(x, magic)) : x; }
+
+struct AttendKernel : AttendArgs {
+  AttendSplit split;
+  uint64_t bt_magic;
+};
+
+// Sequence s of the step, checked; `ok` false: nothing may be read for it.
+struct Seq {
+  int32_t r0, n, cached, ctx;  // first row, new tokens, tokens before, all tokens
+  bool ok;
+};
+__device__ inline Seq sequence(const AttendArgs &a, int32_t s) {
+  Seq q;
+  q.r0 = a.starts[s];
+  const int32_t r1 = a.starts[s + 1];
+  q.cached = a.cached[s];
+  q.n = r1 - q.r0;
+  const int64_t ctx = int64_t(q.cached) + q.n;
+  q.ok = q.r0 >= 0 && r1 >= q.r0 && r1 <= a.max_tokens && q.n <= a.max_fresh && q.cached >= 0 && ctx <= a.max_ctx &&
+         ctx <= int64_t(a.max_blocks) * a.c.bt;
+  q.ctx = int32_t(ctx);
+  return q;
+}
+
+// The first token that any of the sequence's rows from position `pos` on
+// sees, down to a multiple of `align`.
+__device__ inline int32_t first_seen(const AttendArgs &a, int32_t pos, int32_t align) {
+  const int32_t lo = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+  return lo / align * align;
+}
+
+// Local query heads [*h0, *h0 + count) of run j.
+__device__ inline int32_t run_heads(const HeadRuns &h, int32_t j, int32_t *h0) {
+  const int32_t b = max(0, j * h.group - h.cut);
+  *h0 = b;
+  return min(h.n_q, (j + 1) * h.group - h.cut) - b;
+}
+
+// softcap and slope of a score that already has its scale; back in base 2.
+__device__ inline float capped(float score, float cap, float slope, float away) {
+  // tanh(x) = 1 - 2 / (e^2x + 1): off by a few units of 2^-24 of 1, so a score by as many of cap
+  if (cap > 0) score = cap * (1.0f - 2.0f / (__builtin_amdgcn_exp2f(score / cap * (2 * kLog2e)) + 1.0f));
+  return (score + slope * away) * kLog2e;
+}
+
+// 8 values of a 16-bit type with an infinity or NaN among them.
+template <typename T>
+__device__ inline bool not_finite(uint32_t x) {
+  constexpr uint32_t lo = Half16<T>::kExp, hi = Half16<T>::kExp << 16;
+  return (x & lo) == lo || (x & hi) == hi;
+}
+// Each half of x: 1 where it is of the class, else 0 (class 0 NaN, 1 +inf, 2 -inf); class 3: x itself where finite.
+template <typename T, int CLASS>
+__device__ inline uint32_t of_class(uint32_t x) {
+  uint32_t out = 0;
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t v = (x >> (16 * h)) & 0xffff, e = Half16<T>::kExp;
+    const bool big = (v & e) == e, nan = big && (v & Half16<T>::kFrac);
+    const bool in = CLASS == 0 ? nan : CLASS == 1 ? big && !nan && !(v & 0x8000) : CLASS == 2 ? big && !nan && (v & 0x8000) : !big;
+    out |= (in ? CLASS == 3 ? v : Half16<T>::kOne : 0u) << (16 * h);
+  }
+  return out;
+}
+template <typename T, int CLASS>
+__device__ inline typename Half16<T>::v8 of_class(u32x4_t x) {
+  u32x4_t y;
+  for (int i = 0; i < 4; ++i) y[i] = of_class<T, CLASS>(x[i]);
+  return __builtin_bit_cast(typename Half16<T>::v8, y);
+}
+// o with what the weights found of each class.
+__device__ inline float with_classes(float o, float nan, float up, float down) {
+  if (up > 0) o += INFINITY;
+  if (down > 0) o -= INFINITY;
+  return nan > 0 ? NAN : o;
+}
+
+void attend_few(const AttendKernel &a, dim3 grid, hipStream_t st);
+
+}  // namespace atp

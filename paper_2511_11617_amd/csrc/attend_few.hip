@@ -1,0 +1,395 @@
+// attend_few.hip — attention where few rows share a KV head's tokens: one
+// token per sequence, or drafts.  Bound by reading K and V once.
+//
+// One workgroup takes (sequence, run of query heads with one KV head, chunk
+// of the context); its four waves take steps of 32 tokens in turn.  K and V
+// go from memory straight into the operands of the matrix instructions, with
+// no shared memory between:
+//   S^T = K Q^T   operand A: 16 tokens x 32 dimensions, a lane holds 8
+//                 dimensions of one token as they lie in memory
+//   O^T = V^T P^T operand B: the weights, which the lanes hold after the
+//                 first product already: the result's tokens 4 j + i of lane
+//                 group j are taken as the second product's inner index
+//                 (two tiles of 16 tokens side by side), and V is read in the
+//                 same order: a lane reads 8 tokens' values of its dimensions
+//                 and exchanges halves of registers (one permute a dword)
+// A row (token, query head) is a column of both products, so its maximum,
+// sum and scale stay in its lanes.  The maximum moves only when a score
+// passes it by 2^8, so a step has no cross-lane work in general.  The weights
+// enter the second product as a sum of two 16-bit parts (the matrix units
+// idle here): they lose nothing of note.
+#include "attend.h"
+
+namespace atp {
+namespace {
+
+constexpr int kFewWaves = 4;
+constexpr int kStep = 32;
+
+// A lane's 8 dimensions of a K row as an operand.
+template <typename T, typename CT>
+struct KChunk {
+  using raw = u32x4_t;
+  static __device__ typename Half16<T>::v8 operand(raw x) { return __builtin_bit_cast(typename Half16<T>::v8, x); }
+};
+template <typename T>
+struct KChunk<T, E4M3> {
+  using raw = u32x2_t;
+  static __device__ typename Half16<T>::v8 operand(raw x) {
+    const u32x4_t y = {Half16<T>::fp8_lo(x[0]), Half16<T>::fp8_hi(x[0]), Half16<T>::fp8_lo(x[1]), Half16<T>::fp8_hi(x[1])};
+    return __builtin_bit_cast(typename Half16<T>::v8, y);
+  }
+};
+
+template <int BYTES>
+struct Bytes;
+template <>
+struct Bytes<4> { using t = uint32_t; };
+template <>
+struct Bytes<8> { using t = u32x2_t; };
+template <>
+struct Bytes<16> { using t = u32x4_t; };
+
+// N values of a V row (N * sizeof(CT) bytes) as N / 2 dwords of pairs.
+template <typename T, typename CT, int N>
+struct VChunk {
+  using raw = typename Bytes<N * int(sizeof(CT))>::t;
+  static __device__ uint32_t pair(const raw &x, int i) {
+    if constexpr (sizeof(CT) == 2) {
+      return x[i];
+    } else {
+      uint32_t w;
+      if constexpr (sizeof(raw) == 4)
+        w = x;
+      else
+        w = x[i / 2];
+      return i % 2 ? Half16<T>::fp8_hi(w) : Half16<T>::fp8_lo(w);
+    }
+  }
+};
+
+// HD: dimensions the registers hold (head_dim is at most HD); WHOLE: head_dim
+// is HD and block_tokens a multiple of 16, so that a tile of 16 tokens lies
+// in one block and its id is the wave's (scalar); MT: tiles of 16 rows.
+template <typename T, typename CT, int HD, bool WHOLE, int MT>
+__global__ void __launch_bounds__(kFewWaves * 64, 2) k_few(AttendKernel a) {
+  using H = Half16<T>;
+  using v8 = typename H::v8;
+  constexpr int KK = HD / 32, ND = HD / 16, NV = ND < 8 ? ND : 8, VP = ND / NV;
+  using KC = KChunk<T, CT>;
+  using VC = VChunk<T, CT, NV>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
+  const int32_t split = blockIdx.x % a.split.n_split, rest = blockIdx.x / a.split.n_split;
+  const int32_t run = rest % a.h.n_run, s = rest / a.h.n_run;
+  const Seq q = sequence(a, s);
+  if (!q.ok) {
+    if (threadIdx.x == 0) flag(a.status, ATP_EINVAL);
+    return;
+  }
+  if (q.n == 0) return;
+  int32_t h0;
+  const int32_t gh = run_heads(a.h, run, &h0), rows = q.n * gh;
+  const int32_t lo = first_seen(a, q.cached, kStep) + split * a.split.chunk;
+  const int32_t hi = min(q.ctx, lo + a.split.chunk);
+  if (split > 0 && lo >= q.ctx) return;  // the join knows how many chunks there are
+  const int32_t kv = a.h.kv0 + run, hd = a.c.hd;
+  const char *const kbase = a.c.base + int64_t(kv) * a.c.head_stride;
+  const char *const vbase = kbase + a.c.v_off;
+  const int32_t *const table = a.table + int64_t(s) * a.max_blocks;
+  const float ks = a.c.scales ? a.c.scales[kv] : 1.0f, vs = a.c.scales ? a.c.scales[a.c.n_kv + kv] : 1.0f;
+  const bool extras = a.softcap > 0 || a.slopes;
+  const float unit = a.scale * ks * (extras ? 1.0f : kLog2e);
+
+  // rows of this lane: column `col` of each tile
+  int32_t pos[MT];
+  float slope[MT];
+  v8 qf[MT][KK];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int32_t r = min(m * 16 + col, rows - 1), i = r / gh, h = h0 + r % gh;
+    pos[m] = q.cached + i;
+    slope[m] = a.slopes ? a.slopes[h] : 0.0f;
+    const T *src = static_cast<const T *>(a.q) + (q.r0 + i) * a.q_stride + int64_t(h) * hd;
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      const int d = 32 * k + 8 * grp;
+      u32x4_t x = {0, 0, 0, 0};
+      if (m * 16 + col < rows && (WHOLE || d < hd)) x = *reinterpret_cast<const u32x4_t *>(src + d);
+      qf[m][k] = __builtin_bit_cast(v8, x);
+    }
+  }
+  float top[MT], sum[MT];
+  f32x4 o[MT][ND];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    top[m] = -INFINITY;
+    sum[m] = 0;
+#pragma unroll
+    for (int e = 0; e < ND; ++e) o[m][e] = f32x4{0, 0, 0, 0};
+  }
+
+  // What a step reads, and which of its tokens are there (bit per token of
+  // the lane: 4 of each tile).
+  struct Step {
+    typename KC::raw k[2][KK];
+    typename VC::raw v[2][4][VP];
+    uint32_t there;
+  };
+  bool bad = false;
+  auto block_of = [&](int32_t t) -> int32_t {  // t's block id, -1 for none
+    if (t >= hi) return -1;
+    const int32_t p = table[divided(t, a.bt_magic)];
+    if (p < -1 || p >= a.c.num_blocks) bad = true;
+    return uint32_t(p) < uint32_t(a.c.num_blocks) ? p : -1;
+  };
+  auto load = [&](int32_t t0, Step &x) {
+    x.there = 0;
+    if constexpr (WHOLE) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int32_t t = t0 + 16 * u, p = block_of(t);
+        // an absent tile is read from block 0 and masked
+        const int64_t off = p < 0 ? 0 : p * a.c.block_stride + int64_t(t - int32_t(divided(t, a.bt_magic)) * a.c.bt) * a.c.tok_stride;
+        if (p >= 0) x.there |= 0xfu << (4 * u);
+        const char *const kt = kbase + off, *const vt = vbase + off;
+#pragma unroll
+        for (int k = 0; k < KK; ++k)
+          x.k[u][k] = *reinterpret_cast<const typename KC::raw *>(kt + uint32_t(col * a.c.tok_stride + (32 * k + 8 * grp) * int(sizeof(CT))));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < VP; ++c)
+            x.v[u][i][c] = *reinterpret_cast<const typename VC::raw *>(vt + uint32_t((4 * grp + i) * a.c.tok_stride + (col * ND + c * NV) * int(sizeof(CT))));
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int32_t tk = t0 + 16 * u + col, pk = block_of(tk);
+        const int64_t off = pk < 0 ? 0 : pk * a.c.block_stride + int64_t(tk - int32_t(divided(tk, a.bt_magic)) * a.c.bt) * a.c.tok_stride;
+#pragma unroll
+        for (int k = 0; k < KK; ++k) {
+          x.k[u][k] = typename KC::raw{};
+          if (32 * k + 8 * grp < hd)
+            x.k[u][k] = *reinterpret_cast<const typename KC::raw *>(kbase + off + (32 * k + 8 * grp) * int(sizeof(CT)));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int32_t t = t0 + 16 * u + 4 * grp + i, p = block_of(t);
+          const int64_t vo = p < 0 ? 0 : p * a.c.block_stride + int64_t(t - int32_t(divided(t, a.bt_magic)) * a.c.bt) * a.c.tok_stride;
+          if (p >= 0) x.there |= 1u << (4 * u + i);
+#pragma unroll
+          for (int c = 0; c < VP; ++c) {
+            x.v[u][i][c] = typename VC::raw{};
+            if (col * ND + c * NV < hd)
+              x.v[u][i][c] = *reinterpret_cast<const typename VC::raw *>(vbase + vo + (col * ND + c * NV) * int(sizeof(CT)));
+          }
+        }
+      }
+    }
+  };
+
+  auto compute = [&](int32_t t0, const Step &x) {
+    // every row sees every token of the step: the general case
+    const bool whole = t0 + kStep - 1 <= q.cached && t0 + kStep <= hi && __ballot(x.there != 0xff) == 0 &&
+                       (a.window <= 0 || t0 > q.ctx - 1 - a.window);
+    v8 ph[MT], pl[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      f32x4 sc[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        sc[u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < KK; ++k) sc[u] = H::mfma16(KC::operand(x.k[u][k]), qf[m][k], sc[u]);
+      }
+      float z[8], most = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int32_t t = t0 + 16 * (e / 4) + 4 * grp + e % 4;
+        z[e] = sc[e / 4][e % 4] * unit;
+        if (extras) z[e] = capped(z[e], a.softcap, slope[m], float(t - pos[m]));
+        if (!whole) {
+          const bool seen = t <= pos[m] && (a.window <= 0 || pos[m] - t < a.window) && (x.there >> e & 1);
+          z[e] = seen ? z[e] : -INFINITY;
+        }
+        most = fmaxf(most, z[e]);
+      }
+      if (__ballot(most - H::kLift > top[m] + 8.0f)) {
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const float now = fmaxf(top[m], most - H::kLift);
+        const float keep = now == top[m] ? 1.0f : __builtin_amdgcn_exp2f(top[m] - now);
+        top[m] = now;
+        sum[m] *= keep;
+#pragma unroll
+        for (int e = 0; e < ND; ++e) o[m][e] *= keep;
+      }
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = z[e] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(z[e] - top[m]);
+        sum[m] += p[e];
+      }
+      u32x4_t hw, lw;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const typename H::v2 first = {T(p[2 * e]), T(p[2 * e + 1])};
+        hw[e] = __builtin_bit_cast(uint32_t, first);
+        lw[e] = pack2<T>(p[2 * e] - float(first[0]), p[2 * e + 1] - float(first[1]));
+      }
+      ph[m] = __builtin_bit_cast(v8, hw);
+      pl[m] = __builtin_bit_cast(v8, lw);
+    }
+#pragma unroll
+    for (int e = 0; e < ND; ++e) {
+      u32x4_t f;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {  // tokens 2 d, 2 d + 1 of the lane's 8
+        const uint32_t x0 = VC::pair(x.v[d / 2][2 * (d % 2)][e / NV], e % NV / 2);
+        const uint32_t x1 = VC::pair(x.v[d / 2][2 * (d % 2) + 1][e / NV], e % NV / 2);
+        f[d] = e % 2 ? high_halves(x0, x1) : low_halves(x0, x1);
+      }
+      if (!whole && __ballot(not_finite<T>(f[0]) || not_finite<T>(f[1]) || not_finite<T>(f[2]) || not_finite<T>(f[3]))) {
+        // 0 times an unseen infinity or NaN would be NaN: finite values alone go
+        // through the product, and those three classes are counted with the
+        // weights, which are 0 where nothing is seen
+        const f32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          o[m][e] = H::mfma16(of_class<T, 3>(f), ph[m], o[m][e]);
+          o[m][e] = H::mfma16(of_class<T, 3>(f), pl[m], o[m][e]);
+          const f32x4 nan = H::mfma16(of_class<T, 0>(f), ph[m], zero), up = H::mfma16(of_class<T, 1>(f), ph[m], zero),
+                      down = H::mfma16(of_class<T, 2>(f), ph[m], zero);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[m][e][i] = with_classes(o[m][e][i], nan[i], up[i], down[i]);
+        }
+      } else {
+        const v8 vf = __builtin_bit_cast(v8, f);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          o[m][e] = H::mfma16(vf, ph[m], o[m][e]);
+          o[m][e] = H::mfma16(vf, pl[m], o[m][e]);
+        }
+      }
+    }
+  };
+
+  // the next step's reads are in flight while one is computed
+  int32_t t0 = lo + wave * kStep;
+  if (t0 < hi) {
+    Step x;
+    load(t0, x);
+    while (true) {
+      const int32_t t1 = t0 + kFewWaves * kStep;
+      Step y;
+      if (t1 < hi) load(t1, y);
+      compute(t0, x);
+      if (t1 >= hi) break;
+      x = y;
+      t0 = t1;
+    }
+  }
+  if (__ballot(bad) && lane == 0) flag(a.status, ATP_EINVAL);
+
+  // join the four waves through shared memory, then write the rows
+  __shared__ float so[kFewWaves][16][HD + 4];
+  __shared__ float stop[kFewWaves][16], ssum[kFewWaves][16];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    if (m * 16 >= rows) break;
+    if (m) __syncthreads();
+    float l = sum[m];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (grp == 0) {
+      stop[wave][col] = top[m];
+      ssum[wave][col] = l;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < ND; e += 4)  // ND dimensions from (4 grp + i) * ND on
+        *reinterpret_cast<f32x4 *>(&so[wave][col][(4 * grp + i) * ND + e]) = f32x4{o[m][e][i], o[m][e + 1][i], o[m][e + 2][i], o[m][e + 3][i]};
+    __syncthreads();
+    // 16 threads a row, 4 dimensions at a time
+    const int r = threadIdx.x >> 4, part = threadIdx.x & 15;
+    if (m * 16 + r < rows) {
+      float all = -INFINITY, total = 0, f[kFewWaves];
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) all = fmaxf(all, stop[w][r]);
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) {
+        f[w] = stop[w][r] == all ? 1.0f : __builtin_amdgcn_exp2f(stop[w][r] - all);
+        total += f[w] * ssum[w][r];
+      }
+      const float inv = total == 0 ? 0.0f : vs / total;
+      const float lse2 = total == 0 ? -INFINITY : all + __builtin_amdgcn_logf(total);
+      const int32_t i = (m * 16 + r) / gh, h = h0 + (m * 16 + r) % gh;
+      const int64_t row = int64_t(q.r0 + i) * a.h.n_q + h;
+#pragma unroll
+      for (int d = part * 4; d < HD; d += 64) {
+        if (!WHOLE && d >= hd) break;
+        f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) x += *reinterpret_cast<const f32x4 *>(&so[w][r][d]) * f[w];
+        x *= inv;
+        if (a.split.n_split > 1) {
+          *reinterpret_cast<f32x4 *>(a.split.part + (row * a.split.n_split + split) * hd + d) = x;
+        } else {
+          T *dst = static_cast<T *>(a.out) + (q.r0 + i) * a.out_stride + int64_t(h) * hd + d;
+          *reinterpret_cast<u32x2_t *>(dst) = u32x2_t{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3])};
+        }
+      }
+      if (part == 0) {
+        if (a.split.n_split > 1)
+          a.split.part_lse[row * a.split.n_split + split] = lse2;
+        else if (a.lse)
+          a.lse[row] = lse2 * kLn2;
+      }
+    }
+  }
+}
+
+template <typename T, typename CT, int HD, bool WHOLE>
+void launch(const AttendKernel &a, dim3 grid, hipStream_t st) {
+  const dim3 block(kFewWaves * 64);
+  const int64_t rows = int64_t(a.max_fresh) * std::min(a.h.group, a.h.n_q);
+  if (rows <= 16)
+    hipLaunchKernelGGL((k_few<T, CT, HD, WHOLE, 1>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((k_few<T, CT, HD, WHOLE, 2>), grid, block, 0, st, a);
+}
+
+template <typename T, typename CT>
+void by_shape(const AttendKernel &a, dim3 grid, hipStream_t st) {
+  const int hd = a.c.hd;
+  const bool even = a.c.bt % 16 == 0;
+  if (hd == 64 && even)
+    launch<T, CT, 64, true>(a, grid, st);
+  else if (hd == 128 && even)
+    launch<T, CT, 128, true>(a, grid, st);
+  else if (hd == 256 && even)
+    launch<T, CT, 256, true>(a, grid, st);
+  else if (hd <= 64)
+    launch<T, CT, 64, false>(a, grid, st);
+  else if (hd <= 128)
+    launch<T, CT, 128, false>(a, grid, st);
+  else
+    launch<T, CT, 256, false>(a, grid, st);
+}
+
+}  // namespace
+
+void attend_few(const AttendKernel &a, dim3 grid, hipStream_t st) {
+  const bool b = a.dtype == ATP_BF16, e = a.cache_dtype == ATP_E4M3;
+  if (b && e)
+    by_shape<__bf16, E4M3>(a, grid, st);
+  else if (b)
+    by_shape<__bf16, __bf16>(a, grid, st);
+  else if (e)
+    by_shape<_Float16, E4M3>(a, grid, st);
+  else
+    by_shape<_Float16, _Float16>(a, grid, st);
+}
+
+}  // namespace atp

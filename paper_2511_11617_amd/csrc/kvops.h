@@ -82,6 +82,13 @@ struct AttendArgs {
 uint64_t attend_workspace(const AttendArgs &a);
 void attend_launch(const AttendArgs &a, void *ws, void *stream);
 
+// How a call's work is cut: the tokens a sequence sees go in chunks to
+// n_split workgroups, whose results are joined when there are several.
+struct AttendSplit {
+  int32_t chunk, n_split;
+  float *part, *part_lse;  // [rows][query heads][n_split][dim], [..][n_split] (base 2)
+};
+
 // The checks of the entry points (Error on a refusal), before any HIP call.
 void extend_args(const atp_kv_cache *cache, const atp_kv_step *step, ExtendArgs *a);
 void kv_extend(const atp_kv_cache *cache, const atp_kv_step *step, const int32_t *table, void *workspace,

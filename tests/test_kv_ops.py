@@ -202,6 +202,18 @@ def test_attend_mask_and_bound_refusals():
     _refused(atp.EINVAL, "negative bound", _attend, s=_step(max_fresh=-1))
 
 
+def test_attend_workspace_refusals():
+    # one long session: its length is split, so a workspace is needed
+    s = _step(n_seq=1, max_blocks=8192, max_tokens=1, max_fresh=1, max_ctx=131072)
+    n = atp.kv_attend_workspace(_cache(), s)
+    assert n > 0
+    _refused(atp.ECAPACITY, "workspace", _attend, s=s, ws_bytes=n - 1)
+    _refused(atp.EINVAL, "workspace", _attend, s=s, ws=0)
+    _refused(atp.EALIGN, "workspace", _attend, s=s, ws=_addr(9) + 64)
+    for other in (_addr(10), _addr(13), _addr(14), _addr(0)):
+        _refused(atp.EINVAL, "workspace overlaps", _attend, s=s, ws=other)
+
+
 def test_null_descriptions_are_refused():
     L, n, cache, step = atp.lib, C.c_uint64(), _cache(), _step()
     for c, s in ((None, step.ref), (cache.ref, None)):
