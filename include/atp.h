@@ -669,7 +669,7 @@ typedef struct {
  * A block id outside [-1, num_blocks) sets status and counts as -1.  A
  * sequence whose starts, cached or lengths break a bound (max_tokens,
  * max_fresh, max_ctx, max_blocks) sets status and its rows are left as they
- * were.  The result of a call depends on its inputs and bounds alone (sums
+ * were; starts that do not ascend may leave other rows so too.  The result of a call depends on its inputs and bounds alone (sums
  * are taken in a fixed order).  Uses block_table, cached, starts, max_* and
  * status; the workspace size depends on the bounds. */
 int atp_kv_attend_workspace(const atp_kv_cache *cache, const atp_kv_step *step, uint64_t *bytes);

@@ -48,7 +48,7 @@ def build_atp(out_dir: str | None = None, lib_path: str = LIB, defines=()) -> st
         _run(["g++", *HOST_FLAGS, *dflags, "-c", os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
     hip = [(src, os.path.join(out_dir, src + ".o"))
-           for src in ("exec.hip", "kvstep.hip", "attend.hip", "attend_few.hip")]
+           for src in ("exec.hip", "kvstep.hip", "attend.hip", "attend_few.hip", "attend_tile.hip")]
     with ThreadPoolExecutor(len(hip)) as pool:  # the attention kernels' many variants take a minute
         list(pool.map(lambda x: _run([HIPCC, *DEVICE_FLAGS, *dflags, "-c", os.path.join(CSRC, x[0]), "-o", x[1]]), hip))
     objs += [obj for _, obj in hip]

@@ -134,6 +134,9 @@ __device__ inline float with_classes(float o, float nan, float up, float down) {
   return nan > 0 ? NAN : o;
 }
 
+constexpr int kTileRows = 128;  // rows of a workgroup of attend_tile.hip
+
 void attend_few(const AttendKernel &a, dim3 grid, hipStream_t st);
+void attend_tiles(const AttendKernel &a, dim3 grid, int32_t slots, hipStream_t st);
 
 }  // namespace atp

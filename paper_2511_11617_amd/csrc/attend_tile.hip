@@ -1,0 +1,336 @@
+// attend_tile.hip — attention of prompts: many rows share a KV head's
+// tokens.  Bound by the matrix units (4 dim operations per visible pair).
+//
+// One workgroup takes 128 rows of one (sequence, run of query heads with one
+// KV head): row r is token r / heads, head r % heads, so that every row of
+// the tile uses the same K and V.  Four waves hold 32 rows each; tiles of 64
+// tokens of K and V pass through shared memory, two buffers deep, one barrier
+// a tile.  Both products are taken transposed:
+//   S^T = K Q^T (operand A: 32 tokens of K), O^T = V^T P^T (A: 32 dimensions)
+// so a row is a column of both results: its maximum and sum stay in two lanes,
+// and the weights are operand B of the second product where the first left
+// them (the result's token order is the second product's inner order; V is
+// read with the transposing LDS read in that same order).  The maximum moves
+// only when a score passes it by 2^8.
+// K rows are stored with their 16-byte chunks exchanged by the token (chunk
+// ^ token), V rows with their 64-byte parts exchanged by it, so that neither
+// read meets a bank twice; where the cache's elements are the products' own
+// and fill the row, the loads go straight to shared memory (the lane picks
+// the chunk that belongs at its place).
+#include "attend.h"
+
+namespace atp {
+namespace {
+
+constexpr int kTileThreads = 256, kTileTokens = 64;
+
+using lds_ptr = __attribute__((address_space(3))) void *;
+using glb_ptr = const __attribute__((address_space(1))) void *;
+using i16x4 = short __attribute__((ext_vector_type(4)));
+
+template <int HD>
+struct Swizzle {
+  static constexpr int kChunks = HD / 8;  // of 16 bytes, in a row
+  // 16 tokens' equal chunks on 16 places; two rows of 64 dimensions share 256 bytes of banks
+  static __device__ int k(int token) { return HD >= 128 ? token & 15 : (token >> 1) & 7; }
+  static __device__ int v(int token) { return HD >= 128 ? (token & 3) << 2 : ((token >> 1) & 1) << 2; }
+};
+
+template <typename T, typename CT, int HD, bool WHOLE>
+__global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(AttendKernel a, int32_t slots) {
+  using H = Half16<T>;
+  using v8 = typename H::v8;
+  using SW = Swizzle<HD>;
+  constexpr int KK = HD / 16, DT = HD / 32, ROW = HD * 2;
+  constexpr bool DIRECT = WHOLE && sizeof(CT) == 2;
+  constexpr int NCH = kTileTokens * SW::kChunks / kTileThreads;  // chunks a thread stages, of K and of V
+  __shared__ __attribute__((aligned(256))) char lds[2][2][kTileTokens * ROW];
+  __shared__ uint8_t there[2][kTileTokens];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+  // the last slots hold the most tokens: they begin first
+  const int32_t split = blockIdx.x % a.split.n_split, rest = blockIdx.x / a.split.n_split;
+  const int32_t run = rest % a.h.n_run, slot = slots - 1 - rest / a.h.n_run;
+  int32_t h0;
+  const int32_t gh = run_heads(a.h, run, &h0);
+  // sequence s has the slots from starts[s] * heads / 128 + s on
+  int32_t s = 0, hi_s = a.n_seq - 1;
+  while (s < hi_s) {
+    const int32_t mid = (s + hi_s + 1) >> 1;
+    if (int64_t(a.starts[mid]) * gh / kTileRows + mid <= slot)
+      s = mid;
+    else
+      hi_s = mid - 1;
+  }
+  if (rest < a.n_seq && split == 0 && tid == 0 && !sequence(a, rest).ok) flag(a.status, ATP_EINVAL);
+  const Seq q = sequence(a, s);
+  if (!q.ok) return;
+  const int32_t tile = slot - s - int32_t(int64_t(q.r0) * gh / kTileRows), rows = q.n * gh;
+  if (tile < 0 || int64_t(tile) * kTileRows >= rows) return;
+
+  const int32_t kv = a.h.kv0 + run, hd = a.c.hd;
+  const int32_t row0 = tile * kTileRows, rowe = min(rows, row0 + kTileRows) - 1;
+  const int32_t seq_lo = first_seen(a, q.cached, kTileTokens) + split * a.split.chunk;
+  const int32_t lo = max(seq_lo, first_seen(a, q.cached + row0 / gh, kTileTokens));
+  const int32_t hi = min(min(q.ctx, seq_lo + a.split.chunk), q.cached + rowe / gh + 1);
+  const int32_t *const table = a.table + int64_t(s) * a.max_blocks;
+  const char *const kbase = a.c.base + int64_t(kv) * a.c.head_stride;
+  const float ks = a.c.scales ? a.c.scales[kv] : 1.0f, vs = a.c.scales ? a.c.scales[a.c.n_kv + kv] : 1.0f;
+  const bool extras = a.softcap > 0 || a.slopes;
+  const float unit = a.scale * ks * (extras ? 1.0f : kLog2e);
+
+  const int32_t r = min(row0 + wave * 32 + col, rows - 1), tok = r / gh, head = h0 + r % gh, pos = q.cached + tok;
+  const bool mine = row0 + wave * 32 + col < rows;
+  const float slope = a.slopes ? a.slopes[head] : 0.0f;
+  // the wave's first and last position
+  const int32_t wfirst = q.cached + min(row0 + wave * 32, rows - 1) / gh, wlast = q.cached + min(row0 + wave * 32 + 31, rows - 1) / gh;
+  const bool idle = row0 + wave * 32 >= rows;  // it only loads
+  v8 qf[KK];
+  {
+    const T *src = static_cast<const T *>(a.q) + (q.r0 + tok) * a.q_stride + int64_t(head) * hd;
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      u32x4_t x = {0, 0, 0, 0};
+      const int d = 16 * k + 8 * half;
+      if (mine && (WHOLE || d < hd)) x = *reinterpret_cast<const u32x4_t *>(src + d);
+      qf[k] = __builtin_bit_cast(v8, x);
+    }
+  }
+  float top = -INFINITY, sum = 0;
+  f32x16 o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) o[d] = f32x16{};
+
+  bool bad = false;
+  auto block_of = [&](int32_t t) -> int32_t {
+    if (t >= hi) return -1;
+    const int32_t p = table[divided(t, a.bt_magic)];
+    if (p < -1 || p >= a.c.num_blocks) bad = true;
+    return uint32_t(p) < uint32_t(a.c.num_blocks) ? p : -1;
+  };
+  auto offset_of = [&](int32_t t, int32_t p) -> int64_t {
+    return p < 0 ? 0 : p * a.c.block_stride + int64_t(t - int32_t(divided(t, a.bt_magic)) * a.c.bt) * a.c.tok_stride;
+  };
+
+  // Reads a tile of 64 tokens: to shared memory (DIRECT), or to registers that
+  // store() converts and writes.  An absent token is read from block 0.
+  struct Regs {
+    uint32_t x[DIRECT ? 1 : NCH][2][sizeof(CT) == 2 ? 4 : 2];
+    bool here[DIRECT ? 1 : NCH];
+  };
+  auto load = [&](int32_t t0, int buf, Regs &g) {
+    if constexpr (DIRECT) {
+      const int32_t t = t0 + 16 * wave, p = block_of(t);
+      const char *const from = kbase + offset_of(t, p);
+      constexpr int RPI = 1024 / ROW;  // rows of one instruction
+      const int at = lane % SW::kChunks, sub = lane / SW::kChunks;
+#pragma unroll
+      for (int i = 0; i < 16 / RPI; ++i) {
+        const int row = i * RPI + sub;
+        const uint32_t line = row * a.c.tok_stride;
+        char *const to = &lds[buf][0][(16 * wave + i * RPI) * ROW];
+        __builtin_amdgcn_global_load_lds((glb_ptr)(from + line + ((at ^ SW::k(row)) << 4)), (lds_ptr)to, 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((glb_ptr)(from + a.c.v_off + line + ((at ^ SW::v(row)) << 4)),
+                                         (lds_ptr)(to + kTileTokens * ROW), 16, 0, 0);
+      }
+      if (lane < 16) there[buf][16 * wave + lane] = p >= 0;
+    } else {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int idx = i * kTileThreads + tid, row = idx / SW::kChunks, c = idx % SW::kChunks;
+        const int32_t t = t0 + row, p = block_of(t);
+        const char *const from = kbase + offset_of(t, p) + c * 8 * int(sizeof(CT));
+        const bool in = WHOLE || c * 8 < hd;
+        using raw = typename std::conditional<sizeof(CT) == 2, u32x4_t, u32x2_t>::type;
+        raw k = raw{}, v = raw{};
+        if (in) {
+          k = *reinterpret_cast<const raw *>(from);
+          v = *reinterpret_cast<const raw *>(from + a.c.v_off);
+        }
+#pragma unroll
+        for (int j = 0; j < int(sizeof(raw) / 4); ++j) {
+          g.x[i][0][j] = k[j];
+          g.x[i][1][j] = v[j];
+        }
+        g.here[i] = p >= 0;
+      }
+    }
+  };
+  auto store = [&](int buf, const Regs &g) {
+    if constexpr (!DIRECT) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int idx = i * kTileThreads + tid, row = idx / SW::kChunks, c = idx % SW::kChunks;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          u32x4_t y;
+          if constexpr (sizeof(CT) == 2)
+            y = u32x4_t{g.x[i][w][0], g.x[i][w][1], g.x[i][w][2], g.x[i][w][3]};
+          else
+            y = u32x4_t{H::fp8_lo(g.x[i][w][0]), H::fp8_hi(g.x[i][w][0]), H::fp8_lo(g.x[i][w][1]), H::fp8_hi(g.x[i][w][1])};
+          *reinterpret_cast<u32x4_t *>(&lds[buf][w][row * ROW + ((c ^ (w ? SW::v(row) : SW::k(row))) << 4)]) = y;
+        }
+        if (c == 0) there[buf][row] = g.here[i];
+      }
+    }
+  };
+
+  auto compute = [&](int32_t t0, int buf) {
+    const uint64_t seen = __ballot(there[buf][lane] != 0);
+    // every row of the wave sees every token of the tile: the general case
+    const bool whole = t0 + kTileTokens - 1 <= wfirst && seen == ~0ull && (a.window <= 0 || t0 > wlast - a.window);
+    const char *const kl = lds[buf][0], *const vl = lds[buf][1];
+    f32x16 sc[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      sc[u] = f32x16{};
+#pragma unroll
+      for (int k = 0; k < KK; ++k) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t *>(kl + (32 * u + col) * ROW + (((2 * k + half) ^ SW::k(col)) << 4));
+        sc[u] = H::mfma32(__builtin_bit_cast(v8, x), qf[k], sc[u]);
+      }
+    }
+    float most = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int off = 32 * u + 8 * (i / 4) + 4 * half + i % 4;
+        float z = sc[u][i] * unit;
+        if (extras) z = capped(z, a.softcap, slope, float(t0 + off - pos));
+        if (!whole) {
+          const int32_t t = t0 + off;
+          const bool in = t <= pos && (a.window <= 0 || pos - t < a.window) && (seen >> off & 1);
+          z = in ? z : -INFINITY;
+        }
+        sc[u][i] = z;
+        most = fmaxf(most, z);
+      }
+    if (__ballot(most - H::kLift > top + 8.0f)) {
+      most = fmaxf(most, __shfl_xor(most, 32));
+      const float now = fmaxf(top, most - H::kLift);
+      const float keep = now == top ? 1.0f : __builtin_amdgcn_exp2f(top - now);
+      top = now;
+      sum *= keep;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= keep;
+    }
+    // below any score but not -infinity, so that -infinity - it stays -infinity
+    const float ref = top == -INFINITY ? -3.0e38f : top;
+    u32x4_t pw[4];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(sc[u][i] - ref), p1 = __builtin_amdgcn_exp2f(sc[u][i + 1] - ref);
+        sum += p0 + p1;
+        pw[2 * u + i / 8][i % 8 / 2] = pack2<T>(p0, p1);
+      }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        // tokens 16 k + 4 half + (0..3) and 8 further on, of dimension 32 d + lane % 32
+        const int token = 16 * k + 4 * half + (lane & 15) / 4, c = 4 * d + 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
+        const char *const p = vl + token * ROW + ((c ^ SW::v(token)) << 4) + (lane & 1) * 8;
+        const i16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(lds_ptr)p);
+        const i16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(lds_ptr)(p + 8 * ROW));
+        const u32x2_t y0 = __builtin_bit_cast(u32x2_t, x0), y1 = __builtin_bit_cast(u32x2_t, x1);
+        const u32x4_t f = {y0[0], y0[1], y1[0], y1[1]};
+        const v8 pf = __builtin_bit_cast(v8, pw[k]);
+        if (!whole && __ballot(not_finite<T>(f[0]) || not_finite<T>(f[1]) || not_finite<T>(f[2]) || not_finite<T>(f[3]))) {
+          // as in the kernel of few rows: the three classes are counted apart
+          o[d] = H::mfma32(of_class<T, 3>(f), pf, o[d]);
+          const f32x16 nan = H::mfma32(of_class<T, 0>(f), pf, f32x16{});
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[d][i] = with_classes(o[d][i], nan[i], 0, 0);
+          const f32x16 up = H::mfma32(of_class<T, 1>(f), pf, f32x16{});
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[d][i] = with_classes(o[d][i], 0, up[i], 0);
+          const f32x16 down = H::mfma32(of_class<T, 2>(f), pf, f32x16{});
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[d][i] = with_classes(o[d][i], 0, 0, down[i]);
+        } else {
+          o[d] = H::mfma32(__builtin_bit_cast(v8, f), pf, o[d]);
+        }
+      }
+  };
+
+  if (lo < hi) {
+    Regs g;
+    load(lo, 0, g);
+    store(0, g);
+    int buf = 0;
+    for (int32_t t0 = lo; t0 < hi; t0 += kTileTokens, buf ^= 1) {
+      // this tile has come in for every wave, and none reads the other buffer any more
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      const bool more = t0 + kTileTokens < hi;
+      if (more) load(t0 + kTileTokens, buf ^ 1, g);
+      if (!idle && t0 <= wlast && (a.window <= 0 || t0 + kTileTokens > wfirst - a.window + 1)) compute(t0, buf);
+      if (more) store(buf ^ 1, g);
+    }
+  }
+  if (__ballot(bad) && lane == 0) flag(a.status, ATP_EINVAL);
+  sum += __shfl_xor(sum, 32);
+  if (!mine) return;
+  const float inv = sum == 0 ? 0.0f : vs / sum;
+  const float lse2 = sum == 0 ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+  const int64_t row = int64_t(q.r0 + tok) * a.h.n_q + head;
+  const bool parts = a.split.n_split > 1;
+  if (half == 0) {
+    if (parts)
+      a.split.part_lse[row * a.split.n_split + split] = lse2;
+    else if (a.lse)
+      a.lse[row] = lse2 * kLn2;
+  }
+  T *const dst = static_cast<T *>(a.out) + (q.r0 + tok) * a.out_stride + int64_t(head) * hd;
+  float *const part = parts ? a.split.part + (row * a.split.n_split + split) * hd : nullptr;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int at = 32 * d + 2 * i + 4 * half;
+      if (!WHOLE && at >= hd) continue;
+      const f32x4 x = {o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
+      if (parts)
+        *reinterpret_cast<f32x4 *>(part + at) = x;
+      else
+        *reinterpret_cast<u32x2_t *>(dst + at) = u32x2_t{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3])};
+    }
+}
+
+template <typename T, typename CT>
+void by_shape(const AttendKernel &a, dim3 grid, int32_t slots, hipStream_t st) {
+  const dim3 block(kTileThreads);
+  const int hd = a.c.hd;
+  const bool even = a.c.bt % 16 == 0;
+  if (hd == 64 && even)
+    hipLaunchKernelGGL((k_tile<T, CT, 64, true>), grid, block, 0, st, a, slots);
+  else if (hd == 128 && even)
+    hipLaunchKernelGGL((k_tile<T, CT, 128, true>), grid, block, 0, st, a, slots);
+  else if (hd == 256 && even)
+    hipLaunchKernelGGL((k_tile<T, CT, 256, true>), grid, block, 0, st, a, slots);
+  else if (hd <= 64)
+    hipLaunchKernelGGL((k_tile<T, CT, 64, false>), grid, block, 0, st, a, slots);
+  else if (hd <= 128)
+    hipLaunchKernelGGL((k_tile<T, CT, 128, false>), grid, block, 0, st, a, slots);
+  else
+    hipLaunchKernelGGL((k_tile<T, CT, 256, false>), grid, block, 0, st, a, slots);
+}
+
+}  // namespace
+
+void attend_tiles(const AttendKernel &a, dim3 grid, int32_t slots, hipStream_t st) {
+  const bool b = a.dtype == ATP_BF16, e = a.cache_dtype == ATP_E4M3;
+  if (b && e)
+    by_shape<__bf16, E4M3>(a, grid, slots, st);
+  else if (b)
+    by_shape<__bf16, __bf16>(a, grid, slots, st);
+  else if (e)
+    by_shape<_Float16, E4M3>(a, grid, slots, st);
+  else
+    by_shape<_Float16, _Float16>(a, grid, slots, st);
+}
+
+}  // namespace atp

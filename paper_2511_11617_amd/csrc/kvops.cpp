@@ -130,6 +130,7 @@ AttendArgs attend_args(const atp_kv_cache *cache, const atp_kv_step *step) {
   want(step->max_fresh >= 0 && step->max_ctx >= 0, "step: negative bound");
   want(step->max_ctx <= (1 << 30), "step: max_ctx above 2^30");
   want(step->max_fresh <= step->max_ctx || step->n_seq == 0, "step: max_ctx below max_fresh");
+  want(int64_t(step->max_tokens) * a.h.n_q < (int64_t(1) << 31), "step: max_tokens times query heads must fit int32");
   a.c.hd = cache->head_dim;
   a.c.bt = cache->block_tokens;
   a.dtype = cache->dtype;
