@@ -127,6 +127,14 @@ __device__ inline typename Half16<T>::v8 of_class(u32x4_t x) {
   for (int i = 0; i < 4; ++i) y[i] = of_class<T, CLASS>(x[i]);
   return __builtin_bit_cast(typename Half16<T>::v8, y);
 }
+// x with 0 in the place of each half that is no number or no finite one.
+template <typename T>
+__device__ inline uint32_t finite_only(uint32_t x) {
+  constexpr uint32_t e = Half16<T>::kExp;
+  if ((x & e) == e) x &= 0xffff0000u;
+  if ((x & e << 16) == e << 16) x &= 0xffffu;
+  return x;
+}
 // o with what the weights found of each class.
 __device__ inline float with_classes(float o, float nan, float up, float down) {
   if (up > 0) o += INFINITY;

@@ -17,6 +17,8 @@
 // read meets a bank twice; where the cache's elements are the products' own
 // and fill the row, the loads go straight to shared memory (the lane picks
 // the chunk that belongs at its place).
+#include <cfloat>
+
 #include "attend.h"
 
 namespace atp {
@@ -36,7 +38,10 @@ struct Swizzle {
   static __device__ int v(int token) { return HD >= 128 ? (token & 3) << 2 : ((token >> 1) & 1) << 2; }
 };
 
-template <typename T, typename CT, int HD, bool WHOLE>
+// The token of a lane's e-th score of a tile (two results of 16), for the lower half of the lanes; 4 more for the upper.
+__device__ constexpr int token_of(int e) { return 32 * (e / 16) + 8 * (e % 16 / 4) + e % 4; }
+
+template <typename T, typename CT, int HD, bool WHOLE, bool EXTRAS>
 __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(AttendKernel a, int32_t slots) {
   using H = Half16<T>;
   using v8 = typename H::v8;
@@ -70,14 +75,17 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
 
   const int32_t kv = a.h.kv0 + run, hd = a.c.hd;
   const int32_t row0 = tile * kTileRows, rowe = min(rows, row0 + kTileRows) - 1;
+  const int32_t first_pos = q.cached + row0 / gh, last_pos = q.cached + rowe / gh;  // of the workgroup
   const int32_t seq_lo = first_seen(a, q.cached, kTileTokens) + split * a.split.chunk;
-  const int32_t lo = max(seq_lo, first_seen(a, q.cached + row0 / gh, kTileTokens));
-  const int32_t hi = min(min(q.ctx, seq_lo + a.split.chunk), q.cached + rowe / gh + 1);
+  const int32_t lo = max(seq_lo, first_seen(a, first_pos, kTileTokens));
+  const int32_t hi = min(min(q.ctx, seq_lo + a.split.chunk), last_pos + 1);
   const int32_t *const table = a.table + int64_t(s) * a.max_blocks;
   const char *const kbase = a.c.base + int64_t(kv) * a.c.head_stride;
   const float ks = a.c.scales ? a.c.scales[kv] : 1.0f, vs = a.c.scales ? a.c.scales[a.c.n_kv + kv] : 1.0f;
-  const bool extras = a.softcap > 0 || a.slopes;
-  const float unit = a.scale * ks * (extras ? 1.0f : kLog2e);
+  // the scale's sign goes with q, so that the largest product has the largest score
+  // (a scale of 0 makes q 0, so that the unit is positive)
+  const float unit = a.scale == 0 ? 1.0f : fabsf(a.scale) * ks * (EXTRAS ? 1.0f : kLog2e);
+  const uint32_t sign = a.scale < 0 ? 0x80008000u : 0;
 
   const int32_t r = min(row0 + wave * 32 + col, rows - 1), tok = r / gh, head = h0 + r % gh, pos = q.cached + tok;
   const bool mine = row0 + wave * 32 + col < rows;
@@ -92,7 +100,7 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
     for (int k = 0; k < KK; ++k) {
       u32x4_t x = {0, 0, 0, 0};
       const int d = 16 * k + 8 * half;
-      if (mine && (WHOLE || d < hd)) x = *reinterpret_cast<const u32x4_t *>(src + d);
+      if (mine && a.scale != 0 && (WHOLE || d < hd)) x = *reinterpret_cast<const u32x4_t *>(src + d) ^ sign;
       qf[k] = __builtin_bit_cast(v8, x);
     }
   }
@@ -101,6 +109,7 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = f32x16{};
 
+  int32_t left_lo = INT32_MAX, left_hi = 0;  // tokens whose infinities and NaN are still to be added
   bool bad = false;
   auto block_of = [&](int32_t t) -> int32_t {
     if (t >= hi) return -1;
@@ -118,7 +127,7 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
     uint32_t x[DIRECT ? 1 : NCH][2][sizeof(CT) == 2 ? 4 : 2];
     bool here[DIRECT ? 1 : NCH];
   };
-  auto load = [&](int32_t t0, int buf, Regs &g) {
+  auto load = [&](int32_t t0, int buf, Regs &g) __attribute__((always_inline)) {
     if constexpr (DIRECT) {
       const int32_t t = t0 + 16 * wave, p = block_of(t);
       const char *const from = kbase + offset_of(t, p);
@@ -156,7 +165,7 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
       }
     }
   };
-  auto store = [&](int buf, const Regs &g) {
+  auto store = [&](int buf, const Regs &g) __attribute__((always_inline)) {
     if constexpr (!DIRECT) {
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
@@ -175,10 +184,20 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
     }
   };
 
-  auto compute = [&](int32_t t0, int buf) {
-    const uint64_t seen = __ballot(there[buf][lane] != 0);
-    // every row of the wave sees every token of the tile: the general case
-    const bool whole = t0 + kTileTokens - 1 <= wfirst && seen == ~0ull && (a.window <= 0 || t0 > wlast - a.window);
+  // Operand A of the second product: of dimension 32 d + lane % 32, the tokens
+  // 16 k + 4 half + (0..3) and those 8 further on.
+  auto v_operand = [&](const char *vl, int d, int k) __attribute__((always_inline)) {
+    const int token = 16 * k + 4 * half + (lane & 15) / 4, c = 4 * d + 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
+    const char *const p = vl + token * ROW + ((c ^ SW::v(token)) << 4) + (lane & 1) * 8;
+    const i16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(lds_ptr)p);
+    const i16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(lds_ptr)(p + 8 * ROW));
+    const u32x2_t y0 = __builtin_bit_cast(u32x2_t, x0), y1 = __builtin_bit_cast(u32x2_t, x1);
+    return u32x4_t{y0[0], y0[1], y1[0], y1[1]};
+  };
+
+  auto compute = [&](int32_t t0, int buf, uint64_t seen) __attribute__((always_inline)) {
+    // some row of the wave does not see some token of the tile: few tiles of a long context
+    const bool mixed = t0 + kTileTokens - 1 > wfirst || seen != ~0ull || (a.window > 0 && t0 <= wlast - a.window);
     const char *const kl = lds[buf][0], *const vl = lds[buf][1];
     f32x16 sc[2];
 #pragma unroll
@@ -190,22 +209,31 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
         sc[u] = H::mfma32(__builtin_bit_cast(v8, x), qf[k], sc[u]);
       }
     }
-    float most = -INFINITY;
+    // scores in base 2; without extras, still without their unit
+    if (EXTRAS) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+      for (int e = 0; e < 32; ++e)
+        sc[e / 16][e % 16] = capped(sc[e / 16][e % 16] * unit, a.softcap, slope, float(t0 + 4 * half + token_of(e) - pos));
+    }
+    if (mixed) {  // a lane's tokens are t0 + 4 half + token_of(e): seen from the window's begin to its own position
+      const int last = pos - t0 - 4 * half, first = a.window > 0 ? last - a.window : -1;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int off = 32 * u + 8 * (i / 4) + 4 * half + i % 4;
-        float z = sc[u][i] * unit;
-        if (extras) z = capped(z, a.softcap, slope, float(t0 + off - pos));
-        if (!whole) {
-          const int32_t t = t0 + off;
-          const bool in = t <= pos && (a.window <= 0 || pos - t < a.window) && (seen >> off & 1);
-          z = in ? z : -INFINITY;
-        }
-        sc[u][i] = z;
-        most = fmaxf(most, z);
+      for (int e = 0; e < 32; ++e) sc[e / 16][e % 16] = token_of(e) <= last ? sc[e / 16][e % 16] : -INFINITY;
+      if (a.window > 0) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) sc[e / 16][e % 16] = token_of(e) > first ? sc[e / 16][e % 16] : -INFINITY;
       }
+      if (seen != ~0ull) {
+        const uint64_t mine64 = seen >> (4 * half);
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          sc[e / 16][e % 16] = uint32_t(mine64 >> (token_of(e) & 32)) & (1u << (token_of(e) & 31)) ? sc[e / 16][e % 16] : -INFINITY;
+      }
+    }
+    float most = sc[0][0];
+#pragma unroll
+    for (int e = 1; e < 32; ++e) most = fmaxf(most, sc[e / 16][e % 16]);
+    if (!EXTRAS) most *= unit;
     if (__ballot(most - H::kLift > top + 8.0f)) {
       most = fmaxf(most, __shfl_xor(most, 32));
       const float now = fmaxf(top, most - H::kLift);
@@ -219,41 +247,33 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
     const float ref = top == -INFINITY ? -3.0e38f : top;
     u32x4_t pw[4];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int e = 0; e < 32; e += 2) {
+      const float z0 = sc[e / 16][e % 16], z1 = sc[e / 16][e % 16 + 1];
+      const float p0 = __builtin_amdgcn_exp2f(EXTRAS ? z0 - ref : __builtin_fmaf(z0, unit, -ref));
+      const float p1 = __builtin_amdgcn_exp2f(EXTRAS ? z1 - ref : __builtin_fmaf(z1, unit, -ref));
+      sum += p0 + p1;
+      pw[e / 8][e % 8 / 2] = pack2<T>(p0, p1);
+    }
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(sc[u][i] - ref), p1 = __builtin_amdgcn_exp2f(sc[u][i + 1] - ref);
-        sum += p0 + p1;
-        pw[2 * u + i / 8][i % 8 / 2] = pack2<T>(p0, p1);
-      }
+    for (int k = 0; k < 4; ++k)
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        // tokens 16 k + 4 half + (0..3) and 8 further on, of dimension 32 d + lane % 32
-        const int token = 16 * k + 4 * half + (lane & 15) / 4, c = 4 * d + 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
-        const char *const p = vl + token * ROW + ((c ^ SW::v(token)) << 4) + (lane & 1) * 8;
-        const i16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(lds_ptr)p);
-        const i16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(lds_ptr)(p + 8 * ROW));
-        const u32x2_t y0 = __builtin_bit_cast(u32x2_t, x0), y1 = __builtin_bit_cast(u32x2_t, x1);
-        const u32x4_t f = {y0[0], y0[1], y1[0], y1[1]};
-        const v8 pf = __builtin_bit_cast(v8, pw[k]);
-        if (!whole && __ballot(not_finite<T>(f[0]) || not_finite<T>(f[1]) || not_finite<T>(f[2]) || not_finite<T>(f[3]))) {
-          // as in the kernel of few rows: the three classes are counted apart
-          o[d] = H::mfma32(of_class<T, 3>(f), pf, o[d]);
-          const f32x16 nan = H::mfma32(of_class<T, 0>(f), pf, f32x16{});
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] = with_classes(o[d][i], nan[i], 0, 0);
-          const f32x16 up = H::mfma32(of_class<T, 1>(f), pf, f32x16{});
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] = with_classes(o[d][i], 0, up[i], 0);
-          const f32x16 down = H::mfma32(of_class<T, 2>(f), pf, f32x16{});
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] = with_classes(o[d][i], 0, 0, down[i]);
-        } else {
-          o[d] = H::mfma32(__builtin_bit_cast(v8, f), pf, o[d]);
-        }
-      }
+      for (int d = 0; d < DT; ++d)
+        o[d] = H::mfma32(__builtin_bit_cast(v8, v_operand(vl, d, k)), __builtin_bit_cast(v8, pw[k]), o[d]);
+  };
+
+  // 0 times an unseen infinity or NaN would be NaN: in a tile with something
+  // unseen, V's values that are not finite become 0, and what of them is seen
+  // is added behind the last tile.
+  auto clean = [&](int buf) __attribute__((always_inline)) {
+    bool found = false;
+#pragma unroll 1
+    for (int i = tid; i < kTileTokens * ROW / 16; i += kTileThreads) {
+      u32x4_t *const at = reinterpret_cast<u32x4_t *>(&lds[buf][1][i * 16]), x = *at;
+      const bool here = not_finite<T>(x[0]) || not_finite<T>(x[1]) || not_finite<T>(x[2]) || not_finite<T>(x[3]);
+      if (here) *at = u32x4_t{finite_only<T>(x[0]), finite_only<T>(x[1]), finite_only<T>(x[2]), finite_only<T>(x[3])};
+      found |= here;
+    }
+    return __syncthreads_or(found) != 0;
   };
 
   if (lo < hi) {
@@ -265,11 +285,38 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
       // this tile has come in for every wave, and none reads the other buffer any more
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
+      const uint64_t seen = __ballot(there[buf][lane] != 0);
+      if (t0 + kTileTokens - 1 > first_pos || seen != ~0ull || (a.window > 0 && t0 <= last_pos - a.window)) {
+        if (clean(buf)) {
+          left_lo = min(left_lo, t0);
+          left_hi = min(t0 + kTileTokens, hi);
+        }
+      }
       const bool more = t0 + kTileTokens < hi;
       if (more) load(t0 + kTileTokens, buf ^ 1, g);
-      if (!idle && t0 <= wlast && (a.window <= 0 || t0 + kTileTokens > wfirst - a.window + 1)) compute(t0, buf);
+      if (!idle && t0 <= wlast && (a.window <= 0 || t0 + kTileTokens > wfirst - a.window + 1)) compute(t0, buf, seen);
       if (more) store(buf ^ 1, g);
     }
+  }
+  // A seen infinity or NaN (its weight does not matter) makes its dimension
+  // one; those of a tile that all rows saw are in already, and stay the same.
+#pragma unroll 1
+  for (int32_t t = left_lo; t < left_hi; ++t) {
+    const int32_t p = block_of(t);
+    if (p < 0 || t > pos || (a.window > 0 && pos - t >= a.window)) continue;
+    const CT *const v = reinterpret_cast<const CT *>(kbase + a.c.v_off + offset_of(t, p));
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int at = 32 * d + 2 * i + 4 * half;
+        if (!WHOLE && at >= hd) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float x = as_f32(v[at + j]);
+          o[d][i + j] += fabsf(x) <= FLT_MAX ? 0.0f : x;
+        }
+      }
   }
   if (__ballot(bad) && lane == 0) flag(a.status, ATP_EINVAL);
   sum += __shfl_xor(sum, 32);
@@ -300,23 +347,30 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
     }
 }
 
+template <typename T, typename CT, int HD, bool WHOLE>
+void launch(const AttendKernel &a, dim3 grid, int32_t slots, hipStream_t st) {
+  if (a.softcap > 0 || a.slopes)
+    hipLaunchKernelGGL((k_tile<T, CT, HD, WHOLE, true>), grid, dim3(kTileThreads), 0, st, a, slots);
+  else
+    hipLaunchKernelGGL((k_tile<T, CT, HD, WHOLE, false>), grid, dim3(kTileThreads), 0, st, a, slots);
+}
+
 template <typename T, typename CT>
 void by_shape(const AttendKernel &a, dim3 grid, int32_t slots, hipStream_t st) {
-  const dim3 block(kTileThreads);
   const int hd = a.c.hd;
   const bool even = a.c.bt % 16 == 0;
   if (hd == 64 && even)
-    hipLaunchKernelGGL((k_tile<T, CT, 64, true>), grid, block, 0, st, a, slots);
+    launch<T, CT, 64, true>(a, grid, slots, st);
   else if (hd == 128 && even)
-    hipLaunchKernelGGL((k_tile<T, CT, 128, true>), grid, block, 0, st, a, slots);
+    launch<T, CT, 128, true>(a, grid, slots, st);
   else if (hd == 256 && even)
-    hipLaunchKernelGGL((k_tile<T, CT, 256, true>), grid, block, 0, st, a, slots);
+    launch<T, CT, 256, true>(a, grid, slots, st);
   else if (hd <= 64)
-    hipLaunchKernelGGL((k_tile<T, CT, 64, false>), grid, block, 0, st, a, slots);
+    launch<T, CT, 64, false>(a, grid, slots, st);
   else if (hd <= 128)
-    hipLaunchKernelGGL((k_tile<T, CT, 128, false>), grid, block, 0, st, a, slots);
+    launch<T, CT, 128, false>(a, grid, slots, st);
   else
-    hipLaunchKernelGGL((k_tile<T, CT, 256, false>), grid, block, 0, st, a, slots);
+    launch<T, CT, 256, false>(a, grid, slots, st);
 }
 
 }  // namespace
