@@ -90,10 +90,10 @@ __device__ inline int32_t first_seen(const AttendArgs &a, int32_t pos, int32_t a
 }
 
 // Local query heads [*h0, *h0 + count) of run j.
-__device__ inline int32_t run_heads(const HeadRuns &h, int32_t j, int32_t *h0) {
-  const int32_t b = max(0, j * h.group - h.cut);
+__host__ __device__ inline int32_t run_heads(const HeadRuns &h, int32_t j, int32_t *h0) {
+  const int32_t b = j ? j * h.group - h.cut : 0, e = (j + 1) * h.group - h.cut;
   *h0 = b;
-  return min(h.n_q, (j + 1) * h.group - h.cut) - b;
+  return (e < h.n_q ? e : h.n_q) - b;
 }
 
 // softcap and slope of a score that already has its scale; back in base 2.
@@ -144,7 +144,13 @@ __device__ inline float with_classes(float o, float nan, float up, float down) {
 
 constexpr int kTileRows = 128;  // rows of a workgroup of attend_tile.hip
 
+// Places for the tiles of rows of a run of gh heads: sequence s has those
+// from starts[s] * gh / 128 + s on.
+__host__ __device__ inline int64_t tile_slots(const AttendArgs &a, int32_t gh) {
+  return int64_t(a.max_tokens) * gh / kTileRows + a.n_seq;
+}
+
 void attend_few(const AttendKernel &a, dim3 grid, hipStream_t st);
-void attend_tiles(const AttendKernel &a, dim3 grid, int32_t slots, hipStream_t st);
+void attend_tiles(const AttendKernel &a, dim3 grid, hipStream_t st);
 
 }  // namespace atp

@@ -92,16 +92,22 @@ constexpr int32_t kFewLeast = 256, kTileLeast = 512;     // tokens of the shorte
 
 bool few(const AttendArgs &a) { return rows_per_head(a) <= kFewRows; }
 
-// Places for tiles of rows, of one run of heads: starts[s] * heads / 128 + s is sequence s's first.
-int64_t tile_slots(const AttendArgs &a) {
-  return int64_t(a.max_tokens) * std::min(a.h.group, a.h.n_q) / kTileRows + a.n_seq;
+// Workgroups of one chunk that a call takes.
+int64_t groups_of(const AttendArgs &a) {
+  if (few(a)) return int64_t(a.n_seq) * a.h.n_run;
+  int64_t n = 0;
+  for (int32_t j = 0; j < a.h.n_run; ++j) {
+    int32_t h0;
+    n += tile_slots(a, run_heads(a.h, j, &h0));
+  }
+  return n;
 }
 
 // `most`: chunks that no call with these bounds exceeds, whatever its window.
 AttendSplit cut(const AttendArgs &a, int64_t *most) {
   AttendSplit s{0, 1, nullptr, nullptr};
   const int32_t align = few(a) ? kFewAlign : kTileAlign, least = few(a) ? kFewLeast : kTileLeast;
-  const int64_t groups = (few(a) ? int64_t(a.n_seq) : tile_slots(a)) * a.h.n_run, wanted = few(a) ? kFewGroups : kTileGroups;
+  const int64_t groups = groups_of(a), wanted = few(a) ? kFewGroups : kTileGroups;
   const int64_t full = int64_t(a.max_ctx) + align;
   const int64_t span = a.window > 0 ? std::min<int64_t>(full, int64_t(a.window) + a.max_fresh + align) : full;
   const int64_t base = std::max<int64_t>(1, groups), fill = (wanted + base - 1) / base;
@@ -140,15 +146,14 @@ void attend_launch(const AttendArgs &args, void *ws, void *stream) {
   static_cast<AttendArgs &>(a) = args;
   lay_out(args, ws, &a.split);
   a.bt_magic = magic_of(uint32_t(a.c.bt));
-  const int64_t slots = tile_slots(a);
-  const dim3 work = grid_of((few(a) ? a.n_seq : slots) * a.h.n_run * a.split.n_split, 256);
+  const dim3 work = grid_of(groups_of(a) * a.split.n_split, 256);
   // the join takes the rows as they lie: a sequence's are found by its starts
   const dim3 rows = a.split.n_split > 1 ? grid_of(int64_t(a.max_tokens) * a.h.n_q, kJoinThreads) : dim3(1);
   const hipStream_t st = kv_stream(stream);
   if (few(a))
     attend_few(a, work, st);
   else
-    attend_tiles(a, work, int32_t(slots), st);
+    attend_tiles(a, work, st);
   kv_hip(hipGetLastError(), "atp_kv_attend");
   if (a.split.n_split > 1) {
     const int32_t lanes = a.c.hd <= 64 ? 16 : a.c.hd <= 128 ? 32 : 64, align = few(a) ? kFewAlign : kTileAlign;

@@ -42,7 +42,7 @@ struct Swizzle {
 __device__ constexpr int token_of(int e) { return 32 * (e / 16) + 8 * (e % 16 / 4) + e % 4; }
 
 template <typename T, typename CT, int HD, bool WHOLE, bool EXTRAS>
-__global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(AttendKernel a, int32_t slots) {
+__global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(AttendKernel a) {
   using H = Half16<T>;
   using v8 = typename H::v8;
   using SW = Swizzle<HD>;
@@ -53,10 +53,18 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
   __shared__ uint8_t there[2][kTileTokens];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
-  // the last slots hold the most tokens: they begin first
-  const int32_t split = blockIdx.x % a.split.n_split, rest = blockIdx.x / a.split.n_split;
-  const int32_t run = rest % a.h.n_run, slot = slots - 1 - rest / a.h.n_run;
-  int32_t h0;
+  const int32_t split = blockIdx.x % a.split.n_split, item = blockIdx.x / a.split.n_split;
+  // Run by run, so that neighbours, which go to different dies, have alike work;
+  // in a run the last slots begin first: they see the most tokens.
+  int32_t run = 0, slot = item, h0;
+  int32_t n_slots = int32_t(tile_slots(a, run_heads(a.h, 0, &h0)));
+  if (item >= n_slots) {
+    const int32_t each = int32_t(tile_slots(a, a.h.group)), past = item - n_slots;
+    run = min(1 + past / each, a.h.n_run - 1);
+    slot = past - (run - 1) * each;
+    n_slots = int32_t(tile_slots(a, run_heads(a.h, run, &h0)));
+  }
+  slot = n_slots - 1 - slot;
   const int32_t gh = run_heads(a.h, run, &h0);
   // sequence s has the slots from starts[s] * heads / 128 + s on
   int32_t s = 0, hi_s = a.n_seq - 1;
@@ -67,7 +75,7 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
     else
       hi_s = mid - 1;
   }
-  if (rest < a.n_seq && split == 0 && tid == 0 && !sequence(a, rest).ok) flag(a.status, ATP_EINVAL);
+  if (item < a.n_seq && split == 0 && tid == 0 && !sequence(a, item).ok) flag(a.status, ATP_EINVAL);
   const Seq q = sequence(a, s);
   if (!q.ok) return;
   const int32_t tile = slot - s - int32_t(int64_t(q.r0) * gh / kTileRows), rows = q.n * gh;
@@ -348,43 +356,43 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
 }
 
 template <typename T, typename CT, int HD, bool WHOLE>
-void launch(const AttendKernel &a, dim3 grid, int32_t slots, hipStream_t st) {
+void launch(const AttendKernel &a, dim3 grid, hipStream_t st) {
   if (a.softcap > 0 || a.slopes)
-    hipLaunchKernelGGL((k_tile<T, CT, HD, WHOLE, true>), grid, dim3(kTileThreads), 0, st, a, slots);
+    hipLaunchKernelGGL((k_tile<T, CT, HD, WHOLE, true>), grid, dim3(kTileThreads), 0, st, a);
   else
-    hipLaunchKernelGGL((k_tile<T, CT, HD, WHOLE, false>), grid, dim3(kTileThreads), 0, st, a, slots);
+    hipLaunchKernelGGL((k_tile<T, CT, HD, WHOLE, false>), grid, dim3(kTileThreads), 0, st, a);
 }
 
 template <typename T, typename CT>
-void by_shape(const AttendKernel &a, dim3 grid, int32_t slots, hipStream_t st) {
+void by_shape(const AttendKernel &a, dim3 grid, hipStream_t st) {
   const int hd = a.c.hd;
   const bool even = a.c.bt % 16 == 0;
   if (hd == 64 && even)
-    launch<T, CT, 64, true>(a, grid, slots, st);
+    launch<T, CT, 64, true>(a, grid, st);
   else if (hd == 128 && even)
-    launch<T, CT, 128, true>(a, grid, slots, st);
+    launch<T, CT, 128, true>(a, grid, st);
   else if (hd == 256 && even)
-    launch<T, CT, 256, true>(a, grid, slots, st);
+    launch<T, CT, 256, true>(a, grid, st);
   else if (hd <= 64)
-    launch<T, CT, 64, false>(a, grid, slots, st);
+    launch<T, CT, 64, false>(a, grid, st);
   else if (hd <= 128)
-    launch<T, CT, 128, false>(a, grid, slots, st);
+    launch<T, CT, 128, false>(a, grid, st);
   else
-    launch<T, CT, 256, false>(a, grid, slots, st);
+    launch<T, CT, 256, false>(a, grid, st);
 }
 
 }  // namespace
 
-void attend_tiles(const AttendKernel &a, dim3 grid, int32_t slots, hipStream_t st) {
+void attend_tiles(const AttendKernel &a, dim3 grid, hipStream_t st) {
   const bool b = a.dtype == ATP_BF16, e = a.cache_dtype == ATP_E4M3;
   if (b && e)
-    by_shape<__bf16, E4M3>(a, grid, slots, st);
+    by_shape<__bf16, E4M3>(a, grid, st);
   else if (b)
-    by_shape<__bf16, __bf16>(a, grid, slots, st);
+    by_shape<__bf16, __bf16>(a, grid, st);
   else if (e)
-    by_shape<_Float16, E4M3>(a, grid, slots, st);
+    by_shape<_Float16, E4M3>(a, grid, st);
   else
-    by_shape<_Float16, _Float16>(a, grid, slots, st);
+    by_shape<_Float16, _Float16>(a, grid, st);
 }
 
 }  // namespace atp
