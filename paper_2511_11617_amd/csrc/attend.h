@@ -96,11 +96,21 @@ __host__ __device__ inline int32_t run_heads(const HeadRuns &h, int32_t j, int32
   return (e < h.n_q ? e : h.n_q) - b;
 }
 
-// softcap and slope of a score that already has its scale; back in base 2.
-__device__ inline float capped(float score, float cap, float slope, float away) {
-  // tanh(x) = 1 - 2 / (e^2x + 1): off by a few units of 2^-24 of 1, so a score by as many of cap
-  if (cap > 0) score = cap * (1.0f - 2.0f / (__builtin_amdgcn_exp2f(score / cap * (2 * kLog2e)) + 1.0f));
-  return (score + slope * away) * kLog2e;
+// tanh(x) where |x| is at most 0.4: its series to x^11, off by 2^-24 of itself.
+__device__ inline float tanh_small(float x) {
+  const float y = x * x;
+  float p = -1382.0f / 155925.0f;
+  p = __builtin_fmaf(p, y, 62.0f / 2835.0f);
+  p = __builtin_fmaf(p, y, -17.0f / 315.0f);
+  p = __builtin_fmaf(p, y, 2.0f / 15.0f);
+  p = __builtin_fmaf(p, y, -1.0f / 3.0f);
+  return __builtin_fmaf(p * y, x, x);
+}
+constexpr float kTanhSmall = 0.4f;
+// tanh(x) = 1 - 2 / (e^2x + 1), off by a few units of 2^-24 of 1: too much near 0, where the series stands in.
+__device__ inline float tanh_any(float x) {
+  const float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2 * kLog2e)) + 1.0f);
+  return fabsf(x) <= kTanhSmall ? tanh_small(x) : t;
 }
 
 // 8 values of a 16-bit type with an infinity or NaN among them.

@@ -87,7 +87,7 @@ int64_t rows_per_head(const AttendArgs &a) { return int64_t(a.max_fresh) * std::
 constexpr int64_t kFewRows = 32;
 // Chunks of the context begin at multiples of the kernels' steps.
 constexpr int32_t kFewAlign = 32, kTileAlign = 64;
-constexpr int32_t kFewGroups = 1024, kTileGroups = 512;  // workgroups that fill the chip
+constexpr int32_t kFewGroups = 1024, kTileGroups = 1024;  // workgroups that fill the chip
 constexpr int32_t kFewLeast = 256, kTileLeast = 512;     // tokens of the shortest chunk
 
 bool few(const AttendArgs &a) { return rows_per_head(a) <= kFewRows; }

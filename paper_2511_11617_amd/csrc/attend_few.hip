@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kFewWaves * 64, 2) k_few(AttendKernel a) {
   const int32_t *const table = a.table + int64_t(s) * a.max_blocks;
   const float ks = a.c.scales ? a.c.scales[kv] : 1.0f, vs = a.c.scales ? a.c.scales[a.c.n_kv + kv] : 1.0f;
   const bool extras = a.softcap > 0 || a.slopes;
-  const float unit = a.scale * ks * (extras ? 1.0f : kLog2e);
+  const float unit = a.scale * ks * (a.softcap > 0 ? 1.0f / a.softcap : kLog2e), cap2 = a.softcap * kLog2e;
 
   // rows of this lane: column `col` of each tile
   int32_t pos[MT];
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(kFewWaves * 64, 2) k_few(AttendKernel a) {
   for (int m = 0; m < MT; ++m) {
     const int32_t r = min(m * 16 + col, rows - 1), i = r / gh, h = h0 + r % gh;
     pos[m] = q.cached + i;
-    slope[m] = a.slopes ? a.slopes[h] : 0.0f;
+    slope[m] = a.slopes ? a.slopes[h] * kLog2e : 0.0f;
     const T *src = static_cast<const T *>(a.q) + (q.r0 + i) * a.q_stride + int64_t(h) * hd;
 #pragma unroll
     for (int k = 0; k < KK; ++k) {
@@ -207,7 +207,10 @@ __global__ void __launch_bounds__(kFewWaves * 64, 2) k_few(AttendKernel a) {
       for (int e = 0; e < 8; ++e) {
         const int32_t t = t0 + 16 * (e / 4) + 4 * grp + e % 4;
         z[e] = sc[e / 4][e % 4] * unit;
-        if (extras) z[e] = capped(z[e], a.softcap, slope[m], float(t - pos[m]));
+        if (extras) {
+          if (a.softcap > 0) z[e] = cap2 * tanh_any(z[e]);
+          z[e] = __builtin_fmaf(slope[m], float(t - pos[m]), z[e]);
+        }
         if (!whole) {
           const bool seen = t <= pos[m] && (a.window <= 0 || pos[m] - t < a.window) && (x.there >> e & 1);
           z[e] = seen ? z[e] : -INFINITY;

@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
   __shared__ uint8_t there[2][kTileTokens];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
-  const int32_t split = blockIdx.x % a.split.n_split, item = blockIdx.x / a.split.n_split;
+  const int32_t items = gridDim.x / a.split.n_split, split = blockIdx.x / items, item = blockIdx.x % items;
   // Run by run, so that neighbours, which go to different dies, have alike work;
   // in a run the last slots begin first: they see the most tokens.
   int32_t run = 0, slot = item, h0;
@@ -92,12 +92,12 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
   const float ks = a.c.scales ? a.c.scales[kv] : 1.0f, vs = a.c.scales ? a.c.scales[a.c.n_kv + kv] : 1.0f;
   // the scale's sign goes with q, so that the largest product has the largest score
   // (a scale of 0 makes q 0, so that the unit is positive)
-  const float unit = a.scale == 0 ? 1.0f : fabsf(a.scale) * ks * (EXTRAS ? 1.0f : kLog2e);
+  const float unit = a.scale == 0 ? 1.0f : fabsf(a.scale) * ks * (EXTRAS && a.softcap > 0 ? 1.0f / a.softcap : kLog2e);
   const uint32_t sign = a.scale < 0 ? 0x80008000u : 0;
 
   const int32_t r = min(row0 + wave * 32 + col, rows - 1), tok = r / gh, head = h0 + r % gh, pos = q.cached + tok;
   const bool mine = row0 + wave * 32 + col < rows;
-  const float slope = a.slopes ? a.slopes[head] : 0.0f;
+  const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
   // the wave's first and last position
   const int32_t wfirst = q.cached + min(row0 + wave * 32, rows - 1) / gh, wlast = q.cached + min(row0 + wave * 32 + 31, rows - 1) / gh;
   const bool idle = row0 + wave * 32 >= rows;  // it only loads
@@ -219,9 +219,27 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
     }
     // scores in base 2; without extras, still without their unit
     if (EXTRAS) {
+      if (a.softcap > 0) {
+        float x = 0;
 #pragma unroll
-      for (int e = 0; e < 32; ++e)
-        sc[e / 16][e % 16] = capped(sc[e / 16][e % 16] * unit, a.softcap, slope, float(t0 + 4 * half + token_of(e) - pos));
+        for (int e = 0; e < 32; ++e) x = fmaxf(x, fabsf(sc[e / 16][e % 16]));
+        const float cap2 = a.softcap * kLog2e;
+        if (__ballot(!(x * unit <= kTanhSmall)) == 0) {  // most tiles of a cap that is there for outliers
+#pragma unroll
+          for (int e = 0; e < 32; ++e) sc[e / 16][e % 16] = cap2 * tanh_small(sc[e / 16][e % 16] * unit);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) sc[e / 16][e % 16] = cap2 * tanh_any(sc[e / 16][e % 16] * unit);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) sc[e / 16][e % 16] *= unit;
+      }
+      if (a.slopes) {
+        const float from = float(t0 + 4 * half - pos);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) sc[e / 16][e % 16] = __builtin_fmaf(slope, from + float(token_of(e)), sc[e / 16][e % 16]);
+      }
     }
     if (mixed) {  // a lane's tokens are t0 + 4 half + token_of(e): seen from the window's begin to its own position
       const int last = pos - t0 - 4 * half, first = a.window > 0 ? last - a.window : -1;
