@@ -25,8 +25,6 @@ struct Half16<__bf16> {
   using v2 = bf16x2;
   static constexpr float kLift = 0;
   static constexpr uint32_t kExp = 0x7f80;  // exponent bits: all set = infinity or NaN
-  static constexpr uint32_t kFrac = 0x007f;
-  static constexpr uint32_t kOne = 0x3f80;
   static __device__ f32x4 mfma16(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ f32x16 mfma32(v8 a, v8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   static __device__ uint32_t fp8_lo(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false)); }
@@ -38,8 +36,6 @@ struct Half16<_Float16> {
   using v2 = f16x2;
   static constexpr float kLift = 7;
   static constexpr uint32_t kExp = 0x7c00;
-  static constexpr uint32_t kFrac = 0x03ff;
-  static constexpr uint32_t kOne = 0x3c00;
   static __device__ f32x4 mfma16(v8 a, v8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   static __device__ f32x16 mfma32(v8 a, v8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
   static __device__ uint32_t fp8_lo(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, false)); }
@@ -113,29 +109,11 @@ __device__ inline float tanh_any(float x) {
   return fabsf(x) <= kTanhSmall ? tanh_small(x) : t;
 }
 
-// 8 values of a 16-bit type with an infinity or NaN among them.
+// Two values of a 16-bit type with an infinity or NaN among them.
 template <typename T>
 __device__ inline bool not_finite(uint32_t x) {
   constexpr uint32_t lo = Half16<T>::kExp, hi = Half16<T>::kExp << 16;
   return (x & lo) == lo || (x & hi) == hi;
-}
-// Each half of x: 1 where it is of the class, else 0 (class 0 NaN, 1 +inf, 2 -inf); class 3: x itself where finite.
-template <typename T, int CLASS>
-__device__ inline uint32_t of_class(uint32_t x) {
-  uint32_t out = 0;
-  for (int h = 0; h < 2; ++h) {
-    const uint32_t v = (x >> (16 * h)) & 0xffff, e = Half16<T>::kExp;
-    const bool big = (v & e) == e, nan = big && (v & Half16<T>::kFrac);
-    const bool in = CLASS == 0 ? nan : CLASS == 1 ? big && !nan && !(v & 0x8000) : CLASS == 2 ? big && !nan && (v & 0x8000) : !big;
-    out |= (in ? CLASS == 3 ? v : Half16<T>::kOne : 0u) << (16 * h);
-  }
-  return out;
-}
-template <typename T, int CLASS>
-__device__ inline typename Half16<T>::v8 of_class(u32x4_t x) {
-  u32x4_t y;
-  for (int i = 0; i < 4; ++i) y[i] = of_class<T, CLASS>(x[i]);
-  return __builtin_bit_cast(typename Half16<T>::v8, y);
 }
 // x with 0 in the place of each half that is no number or no finite one.
 template <typename T>
@@ -145,13 +123,8 @@ __device__ inline uint32_t finite_only(uint32_t x) {
   if ((x & e << 16) == e << 16) x &= 0xffffu;
   return x;
 }
-// o with what the weights found of each class.
-__device__ inline float with_classes(float o, float nan, float up, float down) {
-  if (up > 0) o += INFINITY;
-  if (down > 0) o -= INFINITY;
-  return nan > 0 ? NAN : o;
-}
-
+// The context's chunks begin at multiples of these.
+constexpr int kFewAlign = 64, kTileAlign = 64;
 constexpr int kTileRows = 128;  // rows of a workgroup of attend_tile.hip
 
 // Places for the tiles of rows of a run of gh heads: sequence s has those

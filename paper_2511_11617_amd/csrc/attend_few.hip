@@ -18,13 +18,18 @@
 // passes it by 2^8, so a step has no cross-lane work in general.  The weights
 // enter the second product as a sum of two 16-bit parts (the matrix units
 // idle here): they lose nothing of note.
+#include <cfloat>
+
 #include "attend.h"
 
 namespace atp {
 namespace {
 
 constexpr int kFewWaves = 4;
-constexpr int kStep = 32;
+// Tokens of a wave's step: 16 KB of K and V at 128 dimensions, in flight while
+// the step before is computed (8-bit steps of 32 tokens read 3.5 TB/s, of 64 4.6).
+template <typename CT, int HD>
+constexpr int kStep = sizeof(CT) == 1 && HD <= 128 ? 64 : 32;
 
 // A lane's 8 dimensions of a K row as an operand.
 template <typename T, typename CT>
@@ -68,14 +73,44 @@ struct VChunk {
   }
 };
 
+// Infinities and NaN of a chunk become 0; whether there were any.
+template <typename T, typename CT>
+__device__ inline bool clean_word(uint32_t &x) {
+  if constexpr (sizeof(CT) == 2) {
+    const uint32_t y = finite_only<T>(x);
+    const bool found = not_finite<T>(x);
+    x = y;
+    return found;
+  } else {
+    const uint32_t nan = ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // bytes of 0x7f or 0xff
+    x &= ~((nan >> 7) * 0xffu);
+    return nan != 0;
+  }
+}
+template <typename T, typename CT, typename V>
+__device__ inline bool clean(V &x) {
+  bool found = false;
+  if constexpr (sizeof(V) == 4) {
+    found = clean_word<T, CT>(x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < int(sizeof(V) / 4); ++i) {
+      uint32_t w = x[i];
+      found |= clean_word<T, CT>(w);
+      x[i] = w;
+    }
+  }
+  return found;
+}
+
 // HD: dimensions the registers hold (head_dim is at most HD); WHOLE: head_dim
 // is HD and block_tokens a multiple of 16, so that a tile of 16 tokens lies
 // in one block and its id is the wave's (scalar); MT: tiles of 16 rows.
 template <typename T, typename CT, int HD, bool WHOLE, int MT>
-__global__ void __launch_bounds__(kFewWaves * 64, 2) k_few(AttendKernel a) {
+__global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT == 2) ? 1 : 2) k_few(AttendKernel a) {
   using H = Half16<T>;
   using v8 = typename H::v8;
-  constexpr int KK = HD / 32, ND = HD / 16, NV = ND < 8 ? ND : 8, VP = ND / NV;
+  constexpr int TS = kStep<CT, HD>, U = TS / 16, KK = HD / 32, ND = HD / 16, NV = ND < 8 ? ND : 8, VP = ND / NV;
   using KC = KChunk<T, CT>;
   using VC = VChunk<T, CT, NV>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
@@ -89,7 +124,7 @@ __global__ void __launch_bounds__(kFewWaves * 64, 2) k_few(AttendKernel a) {
   if (q.n == 0) return;
   int32_t h0;
   const int32_t gh = run_heads(a.h, run, &h0), rows = q.n * gh;
-  const int32_t lo = first_seen(a, q.cached, kStep) + split * a.split.chunk;
+  const int32_t lo = first_seen(a, q.cached, kFewAlign) + split * a.split.chunk;
   const int32_t hi = min(q.ctx, lo + a.split.chunk);
   if (split > 0 && lo >= q.ctx) return;  // the join knows how many chunks there are
   const int32_t kv = a.h.kv0 + run, hd = a.c.hd;
@@ -131,22 +166,23 @@ __global__ void __launch_bounds__(kFewWaves * 64, 2) k_few(AttendKernel a) {
   // What a step reads, and which of its tokens are there (bit per token of
   // the lane: 4 of each tile).
   struct Step {
-    typename KC::raw k[2][KK];
-    typename VC::raw v[2][4][VP];
+    typename KC::raw k[U][KK];
+    typename VC::raw v[U][4][VP];
     uint32_t there;
   };
+  int32_t left_lo = INT32_MAX, left_hi = 0;  // the wave's steps with infinities or NaN still to be added
   bool bad = false;
-  auto block_of = [&](int32_t t) -> int32_t {  // t's block id, -1 for none
+  auto block_of = [&](int32_t t) __attribute__((always_inline)) -> int32_t {  // t's block id, -1 for none
     if (t >= hi) return -1;
     const int32_t p = table[divided(t, a.bt_magic)];
     if (p < -1 || p >= a.c.num_blocks) bad = true;
     return uint32_t(p) < uint32_t(a.c.num_blocks) ? p : -1;
   };
-  auto load = [&](int32_t t0, Step &x) {
+  auto load = [&](int32_t t0, Step &x) __attribute__((always_inline)) {
     x.there = 0;
     if constexpr (WHOLE) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < U; ++u) {
         const int32_t t = t0 + 16 * u, p = block_of(t);
         // an absent tile is read from block 0 and masked
         const int64_t off = p < 0 ? 0 : p * a.c.block_stride + int64_t(t - int32_t(divided(t, a.bt_magic)) * a.c.bt) * a.c.tok_stride;
@@ -163,7 +199,7 @@ __global__ void __launch_bounds__(kFewWaves * 64, 2) k_few(AttendKernel a) {
       }
     } else {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < U; ++u) {
         const int32_t tk = t0 + 16 * u + col, pk = block_of(tk);
         const int64_t off = pk < 0 ? 0 : pk * a.c.block_stride + int64_t(tk - int32_t(divided(tk, a.bt_magic)) * a.c.bt) * a.c.tok_stride;
 #pragma unroll
@@ -188,23 +224,38 @@ __global__ void __launch_bounds__(kFewWaves * 64, 2) k_few(AttendKernel a) {
     }
   };
 
-  auto compute = [&](int32_t t0, const Step &x) {
+  auto compute = [&](int32_t t0, Step &x) __attribute__((always_inline)) {
     // every row sees every token of the step: the general case
-    const bool whole = t0 + kStep - 1 <= q.cached && t0 + kStep <= hi && __ballot(x.there != 0xff) == 0 &&
+    const bool whole = t0 + TS - 1 <= q.cached && t0 + TS <= hi && __ballot(x.there != (1u << 4 * U) - 1) == 0 &&
                        (a.window <= 0 || t0 > q.ctx - 1 - a.window);
-    v8 ph[MT], pl[MT];
+    if (!whole) {
+      // 0 times an unseen infinity or NaN would be NaN: they become 0 here, and
+      // what of them is seen is added behind the last step
+      bool found = false;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < VP; ++c) found |= clean<T, CT>(x.v[u][i][c]);
+      if (__ballot(found)) {
+        left_lo = min(left_lo, t0);
+        left_hi = t0 + TS;
+      }
+    }
+    v8 ph[MT][U / 2], pl[MT][U / 2];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      f32x4 sc[2];
+      f32x4 sc[U];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < U; ++u) {
         sc[u] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < KK; ++k) sc[u] = H::mfma16(KC::operand(x.k[u][k]), qf[m][k], sc[u]);
       }
-      float z[8], most = -INFINITY;
+      float z[4 * U], most = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < 4 * U; ++e) {
         const int32_t t = t0 + 16 * (e / 4) + 4 * grp + e % 4;
         z[e] = sc[e / 4][e % 4] * unit;
         if (extras) {
@@ -227,63 +278,53 @@ __global__ void __launch_bounds__(kFewWaves * 64, 2) k_few(AttendKernel a) {
 #pragma unroll
         for (int e = 0; e < ND; ++e) o[m][e] *= keep;
       }
-      float p[8];
+      float p[4 * U];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < 4 * U; ++e) {
         p[e] = z[e] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(z[e] - top[m]);
         sum[m] += p[e];
       }
-      u32x4_t hw, lw;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const typename H::v2 first = {T(p[2 * e]), T(p[2 * e + 1])};
-        hw[e] = __builtin_bit_cast(uint32_t, first);
-        lw[e] = pack2<T>(p[2 * e] - float(first[0]), p[2 * e + 1] - float(first[1]));
+      for (int g = 0; g < U / 2; ++g) {
+        u32x4_t hw, lw;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p0 = p[8 * g + 2 * e], p1 = p[8 * g + 2 * e + 1];
+          const typename H::v2 first = {T(p0), T(p1)};
+          hw[e] = __builtin_bit_cast(uint32_t, first);
+          lw[e] = pack2<T>(p0 - float(first[0]), p1 - float(first[1]));
+        }
+        ph[m][g] = __builtin_bit_cast(v8, hw);
+        pl[m][g] = __builtin_bit_cast(v8, lw);
       }
-      ph[m] = __builtin_bit_cast(v8, hw);
-      pl[m] = __builtin_bit_cast(v8, lw);
     }
 #pragma unroll
-    for (int e = 0; e < ND; ++e) {
-      u32x4_t f;
+    for (int g = 0; g < U / 2; ++g)
 #pragma unroll
-      for (int d = 0; d < 4; ++d) {  // tokens 2 d, 2 d + 1 of the lane's 8
-        const uint32_t x0 = VC::pair(x.v[d / 2][2 * (d % 2)][e / NV], e % NV / 2);
-        const uint32_t x1 = VC::pair(x.v[d / 2][2 * (d % 2) + 1][e / NV], e % NV / 2);
-        f[d] = e % 2 ? high_halves(x0, x1) : low_halves(x0, x1);
-      }
-      if (!whole && __ballot(not_finite<T>(f[0]) || not_finite<T>(f[1]) || not_finite<T>(f[2]) || not_finite<T>(f[3]))) {
-        // 0 times an unseen infinity or NaN would be NaN: finite values alone go
-        // through the product, and those three classes are counted with the
-        // weights, which are 0 where nothing is seen
-        const f32x4 zero = {0, 0, 0, 0};
+      for (int e = 0; e < ND; ++e) {
+        u32x4_t f;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          o[m][e] = H::mfma16(of_class<T, 3>(f), ph[m], o[m][e]);
-          o[m][e] = H::mfma16(of_class<T, 3>(f), pl[m], o[m][e]);
-          const f32x4 nan = H::mfma16(of_class<T, 0>(f), ph[m], zero), up = H::mfma16(of_class<T, 1>(f), ph[m], zero),
-                      down = H::mfma16(of_class<T, 2>(f), ph[m], zero);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[m][e][i] = with_classes(o[m][e][i], nan[i], up[i], down[i]);
+        for (int d = 0; d < 4; ++d) {  // tokens 2 d, 2 d + 1 of the lane's 8
+          const uint32_t x0 = VC::pair(x.v[2 * g + d / 2][2 * (d % 2)][e / NV], e % NV / 2);
+          const uint32_t x1 = VC::pair(x.v[2 * g + d / 2][2 * (d % 2) + 1][e / NV], e % NV / 2);
+          f[d] = e % 2 ? high_halves(x0, x1) : low_halves(x0, x1);
         }
-      } else {
         const v8 vf = __builtin_bit_cast(v8, f);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          o[m][e] = H::mfma16(vf, ph[m], o[m][e]);
-          o[m][e] = H::mfma16(vf, pl[m], o[m][e]);
+          o[m][e] = H::mfma16(vf, ph[m][g], o[m][e]);
+          o[m][e] = H::mfma16(vf, pl[m][g], o[m][e]);
         }
       }
-    }
   };
 
   // the next step's reads are in flight while one is computed
-  int32_t t0 = lo + wave * kStep;
+  int32_t t0 = lo + wave * TS;
   if (t0 < hi) {
     Step x;
     load(t0, x);
     while (true) {
-      const int32_t t1 = t0 + kFewWaves * kStep;
+      const int32_t t1 = t0 + kFewWaves * TS;
       Step y;
       if (t1 < hi) load(t1, y);
       compute(t0, x);
@@ -292,6 +333,26 @@ __global__ void __launch_bounds__(kFewWaves * 64, 2) k_few(AttendKernel a) {
       t0 = t1;
     }
   }
+#pragma unroll 1
+  for (int32_t t1 = left_lo; t1 < left_hi; t1 += kFewWaves * TS)
+#pragma unroll 1
+    for (int32_t t = t1; t < min(t1 + TS, hi); ++t) {
+      const int32_t p = block_of(t);
+      if (p < 0) continue;
+      const CT *const v = reinterpret_cast<const CT *>(vbase + p * a.c.block_stride + int64_t(t - int32_t(divided(t, a.bt_magic)) * a.c.bt) * a.c.tok_stride);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        if (t > pos[m] || (a.window > 0 && pos[m] - t >= a.window)) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < ND; ++e) {
+            const int d = (4 * grp + i) * ND + e;
+            const float y = WHOLE || d < hd ? as_f32(v[d]) : 0.0f;
+            o[m][e][i] += fabsf(y) <= FLT_MAX ? 0.0f : y;
+          }
+      }
+    }
   if (__ballot(bad) && lane == 0) flag(a.status, ATP_EINVAL);
 
   // join the four waves through shared memory, then write the rows
@@ -357,10 +418,13 @@ template <typename T, typename CT, int HD, bool WHOLE>
 void launch(const AttendKernel &a, dim3 grid, hipStream_t st) {
   const dim3 block(kFewWaves * 64);
   const int64_t rows = int64_t(a.max_fresh) * std::min(a.h.group, a.h.n_q);
-  if (rows <= 16)
-    hipLaunchKernelGGL((k_few<T, CT, HD, WHOLE, 1>), grid, block, 0, st, a);
-  else
-    hipLaunchKernelGGL((k_few<T, CT, HD, WHOLE, 2>), grid, block, 0, st, a);
+  if constexpr (HD <= 128) {  // two tiles of 256 dimensions do not fit the registers
+    if (rows > 16) {
+      hipLaunchKernelGGL((k_few<T, CT, HD, WHOLE, 2>), grid, block, 0, st, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((k_few<T, CT, HD, WHOLE, 1>), grid, block, 0, st, a);
 }
 
 template <typename T, typename CT>

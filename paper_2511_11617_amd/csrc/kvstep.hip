@@ -163,20 +163,40 @@ __global__ void __launch_bounds__(kScanThreads) k_extend_one(ExtendArgs a, Exten
   __syncthreads();
   const int32_t entries = a.n_seq * a.max_blocks;
   bool wrong = false;
-  int32_t at = tid;
-  for (; at + 7 * kScanThreads < entries; at += 8 * kScanThreads) {
-    int32_t p[8];
+  const bool same = a.new_table == a.table;
+  int32_t done = 0;  // entries that the 16-byte reads took
+  if ((reinterpret_cast<uintptr_t>(a.table) | reinterpret_cast<uintptr_t>(a.new_table)) % 16 == 0) {
+    constexpr int kAhead = 4;  // reads in flight in each thread
+    const int32_t quads = entries / 4;
+    for (int32_t q0 = tid; q0 < quads; q0 += kAhead * kScanThreads) {
+      int4 p[kAhead];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) p[j] = a.table[at + j * kScanThreads];
+      for (int j = 0; j < kAhead; ++j) {
+        const int32_t q = q0 + j * kScanThreads;
+        p[j] = q < quads ? reinterpret_cast<const int4 *>(a.table)[q] : int4{-1, -1, -1, -1};
+      }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (a.new_table != a.table) a.new_table[at + j * kScanThreads] = p[j];
-      wrong |= !mark(p[j], a.num_blocks, used, shared);
+      for (int j = 0; j < kAhead; ++j) {
+        const int32_t q = q0 + j * kScanThreads;
+        if (!same && q < quads) reinterpret_cast<int4 *>(a.new_table)[q] = p[j];
+        const int32_t id[4] = {p[j].x, p[j].y, p[j].z, p[j].w};
+        uint32_t old[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool in = uint32_t(id[e]) < uint32_t(a.num_blocks);
+          wrong |= !in && id[e] != -1;
+          old[e] = in ? atomicOr(&used[id[e] >> 5], 1u << (id[e] & 31)) : 0;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (old[e] >> (id[e] & 31) & 1) atomicOr(&shared[id[e] >> 5], 1u << (id[e] & 31));
+      }
     }
+    done = quads * 4;
   }
-  for (; at < entries; at += kScanThreads) {
-    const int32_t p = a.table[at];
-    if (a.new_table != a.table) a.new_table[at] = p;
+  for (int32_t i = done + tid; i < entries; i += kScanThreads) {
+    const int32_t p = a.table[i];
+    if (!same) a.new_table[i] = p;
     wrong |= !mark(p, a.num_blocks, used, shared);
   }
   int64_t tokens = 0;
