@@ -13,7 +13,7 @@ namespace {
 // head; 16, 32 or 64 lanes hold its dimensions, 4 each, and as many groups of
 // lanes take chunks in turn; their sums are added in a fixed order.
 constexpr int kJoinThreads = 256;
-constexpr int kMostSplit = 1024;
+constexpr int kMostSplit = 512;
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) k_join(AttendKernel a, int32_t align, int32_t lanes, bool few_rows) {
   __shared__ float weight[kMostSplit];
@@ -96,7 +96,7 @@ uint64_t magic_of(uint32_t d) { return d <= 1 ? 0 : ~uint64_t(0) / d + 1; }  // 
 // Rows of a KV head that one sequence brings, at most.
 int64_t rows_per_head(const AttendArgs &a) { return int64_t(a.max_fresh) * std::min(a.h.group, a.h.n_q); }
 
-constexpr int32_t kFewGroups = 1024, kTileGroups = 1024;  // workgroups that fill the chip
+constexpr int32_t kFewGroups = 512, kTileGroups = 1024;  // workgroups that fill the chip
 constexpr int32_t kFewLeast = 256, kTileLeast = 512;     // tokens of the shortest chunk
 
 // The kernel of few rows holds two tiles of 16, one of more than 128 dimensions.

@@ -73,6 +73,9 @@ struct VChunk {
   }
 };
 
+// The token of a lane's e-th score of a step, from its group's first on.
+__device__ constexpr int token_of(int e) { return 16 * (e / 4) + e % 4; }
+
 // Infinities and NaN of a chunk become 0; whether there were any.
 template <typename T, typename CT>
 __device__ inline bool clean_word(uint32_t &x) {
@@ -132,7 +135,6 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
   const char *const vbase = kbase + a.c.v_off;
   const int32_t *const table = a.table + int64_t(s) * a.max_blocks;
   const float ks = a.c.scales ? a.c.scales[kv] : 1.0f, vs = a.c.scales ? a.c.scales[a.c.n_kv + kv] : 1.0f;
-  const bool extras = a.softcap > 0 || a.slopes;
   const float unit = a.scale * ks * (a.softcap > 0 ? 1.0f / a.softcap : kLog2e), cap2 = a.softcap * kLog2e;
 
   // rows of this lane: column `col` of each tile
@@ -253,21 +255,30 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
 #pragma unroll
         for (int k = 0; k < KK; ++k) sc[u] = H::mfma16(KC::operand(x.k[u][k]), qf[m][k], sc[u]);
       }
-      float z[4 * U], most = -INFINITY;
+      // the lane's tokens are t0 + 4 grp + token_of(e)
+      float z[4 * U];
 #pragma unroll
-      for (int e = 0; e < 4 * U; ++e) {
-        const int32_t t = t0 + 16 * (e / 4) + 4 * grp + e % 4;
-        z[e] = sc[e / 4][e % 4] * unit;
-        if (extras) {
-          if (a.softcap > 0) z[e] = cap2 * tanh_any(z[e]);
-          z[e] = __builtin_fmaf(slope[m], float(t - pos[m]), z[e]);
-        }
-        if (!whole) {
-          const bool seen = t <= pos[m] && (a.window <= 0 || pos[m] - t < a.window) && (x.there >> e & 1);
+      for (int e = 0; e < 4 * U; ++e) z[e] = sc[e / 4][e % 4] * unit;
+      if (a.softcap > 0) {
+#pragma unroll
+        for (int e = 0; e < 4 * U; ++e) z[e] = cap2 * tanh_any(z[e]);
+      }
+      if (a.slopes) {
+        const float from = float(t0 + 4 * grp - pos[m]);
+#pragma unroll
+        for (int e = 0; e < 4 * U; ++e) z[e] = __builtin_fmaf(slope[m], from + float(token_of(e)), z[e]);
+      }
+      if (!whole) {
+        const int last = pos[m] - t0 - 4 * grp, first = a.window > 0 ? last - a.window : -1;
+#pragma unroll
+        for (int e = 0; e < 4 * U; ++e) {
+          const bool seen = bool(token_of(e) <= last) & bool(token_of(e) > first) & bool(x.there >> e & 1);
           z[e] = seen ? z[e] : -INFINITY;
         }
-        most = fmaxf(most, z[e]);
       }
+      float most = z[0];
+#pragma unroll
+      for (int e = 1; e < 4 * U; ++e) most = fmaxf(most, z[e]);
       if (__ballot(most - H::kLift > top[m] + 8.0f)) {
         most = fmaxf(most, __shfl_xor(most, 16));
         most = fmaxf(most, __shfl_xor(most, 32));
@@ -278,10 +289,12 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
 #pragma unroll
         for (int e = 0; e < ND; ++e) o[m][e] *= keep;
       }
+      // below any score but not -infinity, so that -infinity - it stays -infinity
+      const float ref = top[m] == -INFINITY ? -3.0e38f : top[m];
       float p[4 * U];
 #pragma unroll
       for (int e = 0; e < 4 * U; ++e) {
-        p[e] = z[e] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(z[e] - top[m]);
+        p[e] = __builtin_amdgcn_exp2f(z[e] - ref);
         sum[m] += p[e];
       }
 #pragma unroll
