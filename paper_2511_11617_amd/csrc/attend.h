@@ -125,6 +125,7 @@ __device__ inline uint32_t finite_only(uint32_t x) {
 }
 // The context's chunks begin at multiples of these.
 constexpr int kFewAlign = 64, kTileAlign = 64;
+constexpr int kFewLeast = 256;  // tokens of the shortest chunk of few rows
 constexpr int kTileRows = 128;  // rows of a workgroup of attend_tile.hip
 
 // Places for the tiles of rows of a run of gh heads: sequence s has those

@@ -106,6 +106,79 @@ __device__ inline bool clean(V &x) {
   return found;
 }
 
+// The chunk of a workgroup.  Every workgroup sums the sequences' spans, which
+// gives the chunks' length (groups of them over all, none shorter than
+// kFewLeast), counts the chunks before each sequence and finds its own: the
+// work is even whatever the lengths, and the host need not know them.
+// Workgroup w takes run w % n_run of chunk w / n_run.
+struct Share {
+  int32_t s, lo, hi, count;  // count: chunks of the sequence; s < 0: none
+};
+__device__ inline Share share_of(const AttendKernel &a) {
+  constexpr int T = kFewWaves * 64;
+  __shared__ int64_t total64[kFewWaves];
+  __shared__ int32_t sums[kFewWaves], mine[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int64_t total = 0;
+  int32_t span0 = 0, from0 = 0;  // of this thread's first sequence: most steps have no more than threads
+  for (int32_t s = tid; s < a.n_seq; s += T) {
+    const Seq q = sequence(a, s);
+    if (!q.ok && blockIdx.x == 0) flag(a.status, ATP_EINVAL);
+    const int32_t from = q.ok ? first_seen(a, q.cached, kFewAlign) : 0, span = q.ok && q.n ? q.ctx - from : 0;
+    if (s == tid) {
+      span0 = span;
+      from0 = from;
+    }
+    total += span;
+  }
+  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+  if (lane == 0) total64[wave] = total;
+  if (tid == 0) mine[0] = -1;
+  __syncthreads();
+  total = 0;
+  for (int w = 0; w < kFewWaves; ++w) total += total64[w];
+  const int64_t each = (total * a.h.n_run + a.split.groups - 1) / a.split.groups;
+  const int32_t chunk = int32_t((min(max(each, int64_t(kFewLeast)), int64_t(1) << 30) + kFewAlign - 1) / kFewAlign * kFewAlign);
+  const int32_t want = blockIdx.x / a.h.n_run;
+  int32_t before = 0;
+  for (int32_t s0 = 0; s0 < a.n_seq && (before <= want || blockIdx.x == 0); s0 += T) {
+    const int32_t s = s0 + tid;
+    int32_t span = span0, from = from0;
+    if (s0 && s < a.n_seq) {
+      const Seq q = sequence(a, s);
+      from = q.ok ? first_seen(a, q.cached, kFewAlign) : 0;
+      span = q.ok && q.n ? q.ctx - from : 0;
+    }
+    const int32_t n = s < a.n_seq ? (span + chunk - 1) / chunk : 0;
+    int32_t inc = n;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int32_t y = __shfl_up(inc, d);
+      if (lane >= d) inc += y;
+    }
+    if (s0) __syncthreads();
+    if (lane == 63) sums[wave] = inc;
+    __syncthreads();
+    int32_t at = before + inc - n;
+    for (int w = 0; w < kFewWaves; ++w) {
+      if (w < wave) at += sums[w];
+      before += sums[w];
+    }
+    if (want >= at && want < at + n) {
+      mine[0] = s;
+      mine[1] = from + (want - at) * chunk;
+      mine[2] = int32_t(min(int64_t(from) + span, int64_t(mine[1]) + chunk));
+      mine[3] = n;
+    }
+    if (blockIdx.x == 0 && s < a.n_seq && a.split.shares) {  // for the join
+      a.split.shares[2 * s] = at;
+      a.split.shares[2 * s + 1] = n;
+    }
+  }
+  __syncthreads();
+  return {__builtin_amdgcn_readfirstlane(mine[0]), __builtin_amdgcn_readfirstlane(mine[1]), __builtin_amdgcn_readfirstlane(mine[2]),
+          __builtin_amdgcn_readfirstlane(mine[3])};
+}
+
 // HD: dimensions the registers hold (head_dim is at most HD); WHOLE: head_dim
 // is HD and block_tokens a multiple of 16, so that a tile of 16 tokens lies
 // in one block and its id is the wave's (scalar); MT: tiles of 16 rows.
@@ -117,19 +190,13 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
   using KC = KChunk<T, CT>;
   using VC = VChunk<T, CT, NV>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
-  const int32_t split = blockIdx.x % a.split.n_split, rest = blockIdx.x / a.split.n_split;
-  const int32_t run = rest % a.h.n_run, s = rest / a.h.n_run;
+  const Share sh = share_of(a);
+  if (sh.s < 0) return;
+  const int32_t run = blockIdx.x % a.h.n_run, s = sh.s;
   const Seq q = sequence(a, s);
-  if (!q.ok) {
-    if (threadIdx.x == 0) flag(a.status, ATP_EINVAL);
-    return;
-  }
-  if (q.n == 0) return;
   int32_t h0;
   const int32_t gh = run_heads(a.h, run, &h0), rows = q.n * gh;
-  const int32_t lo = first_seen(a, q.cached, kFewAlign) + split * a.split.chunk;
-  const int32_t hi = min(q.ctx, lo + a.split.chunk);
-  if (split > 0 && lo >= q.ctx) return;  // the join knows how many chunks there are
+  const int32_t lo = sh.lo, hi = sh.hi;
   const int32_t kv = a.h.kv0 + run, hd = a.c.hd;
   const char *const kbase = a.c.base + int64_t(kv) * a.c.head_stride;
   const char *const vbase = kbase + a.c.v_off;
@@ -410,16 +477,16 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
 #pragma unroll
         for (int w = 0; w < kFewWaves; ++w) x += *reinterpret_cast<const f32x4 *>(&so[w][r][d]) * f[w];
         x *= inv;
-        if (a.split.n_split > 1) {
-          *reinterpret_cast<f32x4 *>(a.split.part + (row * a.split.n_split + split) * hd + d) = x;
+        if (sh.count > 1) {
+          *reinterpret_cast<f32x4 *>(a.split.part + (int64_t(blockIdx.x) * a.split.n_split + m * 16 + r) * hd + d) = x;
         } else {
           T *dst = static_cast<T *>(a.out) + (q.r0 + i) * a.out_stride + int64_t(h) * hd + d;
           *reinterpret_cast<u32x2_t *>(dst) = u32x2_t{pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3])};
         }
       }
       if (part == 0) {
-        if (a.split.n_split > 1)
-          a.split.part_lse[row * a.split.n_split + split] = lse2;
+        if (sh.count > 1)
+          a.split.part_lse[int64_t(blockIdx.x) * a.split.n_split + m * 16 + r] = lse2;
         else if (a.lse)
           a.lse[row] = lse2 * kLn2;
       }

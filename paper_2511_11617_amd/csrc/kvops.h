@@ -82,11 +82,15 @@ struct AttendArgs {
 uint64_t attend_workspace(const AttendArgs &a);
 void attend_launch(const AttendArgs &a, void *ws, void *stream);
 
-// How a call's work is cut: the tokens a sequence sees go in chunks to
-// n_split workgroups, whose results are joined when there are several.
+// How a call's context is cut over workgroups whose results are joined.
+//   many rows  chunk k of every sequence's tokens begins `chunk` tokens behind
+//              chunk k - 1; n_split chunks at most
+//   few rows   the chunks' length is found on the device, for about `groups`
+//              of them over all sequences; workgroup w has the results' place w
 struct AttendSplit {
-  int32_t chunk, n_split;
-  float *part, *part_lse;  // [rows][query heads][n_split][dim], [..][n_split] (base 2)
+  int32_t chunk, n_split, groups;
+  float *part, *part_lse;  // [rows][query heads][n_split][dim], [..][n_split] (base 2); few: [w][rows][dim], [w][rows]
+  int32_t *shares;         // few: [n_seq][2], a sequence's first chunk and their number
 };
 
 // The checks of the entry points (Error on a refusal), before any HIP call.
