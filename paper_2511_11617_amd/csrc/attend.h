@@ -134,6 +134,37 @@ __host__ __device__ inline int64_t tile_slots(const AttendArgs &a, int32_t gh) {
   return int64_t(a.max_tokens) * gh / kTileRows + a.n_seq;
 }
 
+#if defined(__HIPCC__)
+// The tile of rows that is number `item` of a call's, run by run (so that
+// neighbours, which go to different dies, have alike work), and in a run from
+// the last slot to the first; s < 0: none.
+__device__ inline TileItem tile_of(const AttendArgs &a, int32_t item) {
+  int32_t run = 0, slot = item, h0;
+  int32_t n_slots = int32_t(tile_slots(a, run_heads(a.h, 0, &h0)));
+  if (item >= n_slots) {
+    const int32_t each = int32_t(tile_slots(a, a.h.group)), past = item - n_slots;
+    run = min(1 + past / each, a.h.n_run - 1);
+    slot = past - (run - 1) * each;
+    n_slots = int32_t(tile_slots(a, run_heads(a.h, run, &h0)));
+  }
+  slot = n_slots - 1 - slot;
+  const int32_t gh = run_heads(a.h, run, &h0);
+  int32_t s = 0, hi_s = a.n_seq - 1;  // the last sequence whose slots begin at or before this one
+  while (s < hi_s) {
+    const int32_t mid = (s + hi_s + 1) >> 1;
+    if (int64_t(a.starts[mid]) * gh / kTileRows + mid <= slot)
+      s = mid;
+    else
+      hi_s = mid - 1;
+  }
+  const Seq q = sequence(a, s);
+  const int32_t tile = slot - s - int32_t(int64_t(q.r0) * gh / kTileRows), rows = q.n * gh;
+  if (!q.ok || tile < 0 || int64_t(tile) * kTileRows >= rows) return {-1, 0, 0, 0, 0, -1};
+  const int32_t row0 = tile * kTileRows, rowe = min(rows, row0 + kTileRows) - 1;
+  return {s, run, tile, first_seen(a, q.cached + row0 / gh, kTileAlign), q.cached + rowe / gh + 1, -1};
+}
+#endif
+
 void attend_few(const AttendKernel &a, dim3 grid, hipStream_t st);
 void attend_tiles(const AttendKernel &a, dim3 grid, hipStream_t st);
 

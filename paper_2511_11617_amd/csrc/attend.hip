@@ -9,52 +9,29 @@ namespace atp {
 namespace {
 
 // Joins a row's chunks: out = sum 2^(lse_c - max) out_c / sum 2^(lse_c - max),
-// each chunk's out_c being its own weighted mean.  One workgroup per row and
-// head; 16, 32 or 64 lanes hold its dimensions, 4 each, and as many groups of
-// lanes take chunks in turn; their sums are added in a fixed order.
+// each chunk's out_c being its own weighted mean, in a fixed order.
+
+// Few rows: one workgroup per row and head; 16, 32 or 64 lanes hold its
+// dimensions, 4 each, and as many groups of lanes take chunks in turn.
 constexpr int kJoinThreads = 256;
 constexpr int kMostSplit = 1024;
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) k_join(AttendKernel a, int32_t lanes, bool few_rows) {
+__global__ void __launch_bounds__(kJoinThreads) k_join(AttendKernel a, int32_t lanes) {
   __shared__ float weight[kMostSplit];
   __shared__ float red[kJoinThreads / 64], red2[kJoinThreads / 64];
   __shared__ f32x4 acc[kJoinThreads];
-  const int32_t item = blockIdx.x, h = item % a.h.n_q, at_row = item / a.h.n_q;
-  int32_t s, i;
-  if (few_rows) {  // a place for each sequence's most rows
-    s = at_row / a.max_fresh;
-    i = at_row % a.max_fresh;
-  } else {  // the rows as they lie: the last sequence that starts at or before this one
-    s = 0;
-    for (int32_t hi = a.n_seq - 1; s < hi;) {
-      const int32_t mid = (s + hi + 1) >> 1;
-      if (a.starts[mid] <= at_row)
-        s = mid;
-      else
-        hi = mid - 1;
-    }
-    i = at_row - a.starts[s];
-  }
+  const int32_t item = blockIdx.x, h = item % a.h.n_q, i = item / a.h.n_q % a.max_fresh, s = item / a.h.n_q / a.max_fresh;
   const Seq q = sequence(a, s);
-  if (!q.ok || i < 0 || i >= q.n) return;
+  if (!q.ok || i >= q.n) return;
   const int tid = threadIdx.x, groups = blockDim.x / lanes, waves = blockDim.x / 64;
   const int64_t row = int64_t(q.r0 + i) * a.h.n_q + h;
-  int32_t chunks;
-  int64_t first, step;  // places of the row's chunks
-  if (few_rows) {
-    chunks = a.split.shares[2 * s + 1];
-    if (chunks <= 1) return;  // written already
-    const int32_t run = (h + a.h.cut) / a.h.group;
-    int32_t h0;
-    const int32_t gh = run_heads(a.h, run, &h0);
-    step = int64_t(a.h.n_run) * a.split.n_split;
-    first = (int64_t(a.split.shares[2 * s]) * a.h.n_run + run) * a.split.n_split + i * gh + h - h0;
-  } else {
-    const int32_t span = q.ctx - first_seen(a, q.cached, kTileAlign);
-    chunks = min(a.split.n_split, max(1, (span + a.split.chunk - 1) / a.split.chunk));
-    step = 1;
-    first = row * a.split.n_split;
-  }
+  const int32_t chunks = a.split.shares[2 * s + 1];
+  if (chunks <= 1) return;  // written already
+  const int32_t run = (h + a.h.cut) / a.h.group;
+  int32_t h0;
+  const int32_t gh = run_heads(a.h, run, &h0);
+  const int64_t step = int64_t(a.h.n_run) * a.split.n_split;  // from chunk to chunk
+  const int64_t first = (int64_t(a.split.shares[2 * s]) * a.h.n_run + run) * a.split.n_split + i * gh + h - h0;
   const float *lse = a.split.part_lse + first;
   float most = -INFINITY, total = 0;
   for (int c = tid; c < chunks; c += blockDim.x) {
@@ -105,13 +82,129 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(AttendKernel a, int32_t l
   if (tid == 0 && a.lse) a.lse[row] = total == 0 ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
+// Many rows: a workgroup takes 16 rows of a cut tile; `lanes` lanes a row.
+constexpr int kJoinRows = 16;
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) k_join_tiles(AttendKernel a, int32_t lanes) {
+  const int32_t item = blockIdx.x / (kTileRows / kJoinRows), part = blockIdx.x % (kTileRows / kJoinRows);
+  const int32_t place = a.split.cuts[2 * item], parts = a.split.cuts[2 * item + 1];
+  if (parts <= 1) return;
+  const TileItem t = tile_of(a, item);
+  const Seq q = sequence(a, t.s);
+  int32_t h0;
+  const int32_t gh = run_heads(a.h, t.run, &h0), rows = q.n * gh, hd = a.c.hd;
+  const int at = threadIdx.x % lanes, d = at * 4, each = kJoinThreads / lanes;
+  for (int32_t x = threadIdx.x / lanes; x < kJoinRows; x += each) {
+    const int32_t in = part * kJoinRows + x, r = t.tile * kTileRows + in;
+    if (r >= rows) break;
+    const float *lse = a.split.part_lse + int64_t(place) * kTileRows + in;
+    float most = -INFINITY, total = 0;
+    for (int c = at; c < parts; c += lanes) most = fmaxf(most, lse[int64_t(c) * kTileRows]);
+    for (int e = lanes / 2; e; e >>= 1) most = fmaxf(most, __shfl_xor(most, e));
+    const float base = most == -INFINITY ? 0.0f : most;
+    f32x4 o = {0, 0, 0, 0};
+    constexpr int kAhead = 4;
+    for (int c0 = 0; c0 < parts; c0 += kAhead) {
+      f32x4 y[kAhead];
+      float w[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int64_t from = (int64_t(place) + c0 + j) * kTileRows + in;
+        w[j] = c0 + j < parts ? a.split.part_lse[from] : -INFINITY;
+        y[j] = f32x4{0, 0, 0, 0};
+        if (c0 + j < parts && d < hd) y[j] = *reinterpret_cast<const f32x4 *>(a.split.part + from * hd + d);
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const float v = __builtin_amdgcn_exp2f(w[j] - base);
+        total += v;
+        o += v * y[j];
+      }
+    }
+    const float inv = total == 0 ? 0.0f : 1.0f / total;
+    const int32_t i = r / gh, h = h0 + r % gh;
+    if (d < hd) {
+      T *dst = static_cast<T *>(a.out) + (q.r0 + i) * a.out_stride + int64_t(h) * hd + d;
+      *reinterpret_cast<u32x2_t *>(dst) = u32x2_t{pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv)};
+    }
+    if (at == 0 && a.lse) a.lse[int64_t(q.r0 + i) * a.h.n_q + h] = total == 0 ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
+  }
+}
+
+// The list of many rows' work, by one workgroup: tiles longer than the chip's
+// share (their tokens over kTileParts) are cut into equal parts, and all go
+// into the list longest first (32 classes of length), so that the last ones to
+// begin are short.
+constexpr int kListThreads = 1024, kListTiles = 4096, kClasses = 32;
+constexpr int32_t kTileParts = 1024, kTileLeast = 512;
+__global__ void __launch_bounds__(kListThreads) k_list_tiles(AttendKernel a, bool cut) {
+  constexpr int kEach = kListTiles / kListThreads;
+  __shared__ int64_t sums[kListThreads / 64];
+  __shared__ int32_t count[kClasses], from[kClasses], places, n;
+  const int tid = threadIdx.x;
+  for (int32_t s = tid; s < a.n_seq; s += kListThreads)
+    if (!sequence(a, s).ok) flag(a.status, ATP_EINVAL);
+  TileItem t[kEach];
+  int64_t total = 0;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int32_t item = j * kListThreads + tid;
+    t[j].s = -1;
+    if (item < a.split.tiles) t[j] = tile_of(a, item);
+    if (t[j].s >= 0) total += t[j].hi - t[j].lo;
+  }
+  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+  if ((tid & 63) == 0) sums[tid >> 6] = total;
+  if (tid < kClasses) count[tid] = 0;
+  if (tid == 0) places = n = 0;
+  __syncthreads();
+  total = 0;
+  for (int w = 0; w < kListThreads / 64; ++w) total += sums[w];
+  int32_t most = int32_t(min(max((total + kTileParts - 1) / kTileParts, int64_t(kTileLeast)), int64_t(1) << 30));
+  if (!cut) most = 1 << 30;
+  const int32_t scale = cut ? most : int32_t(min(int64_t(a.max_ctx), int64_t(1) << 30));
+  int32_t parts[kEach], length[kEach], at[kEach];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    parts[j] = 0;
+    if (t[j].s < 0) continue;
+    const int32_t span = t[j].hi - t[j].lo, want = (span + most - 1) / most;
+    length[j] = ((span + want - 1) / want + kTileAlign - 1) / kTileAlign * kTileAlign;
+    parts[j] = (span + length[j] - 1) / length[j];
+    // class 0 is the longest
+    const int32_t cls = kClasses - 1 - int32_t(min(int64_t(length[j]) * kClasses / (int64_t(scale) + 1), int64_t(kClasses - 1)));
+    at[j] = cls << 24 | atomicAdd(&count[cls], parts[j]);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    int32_t sum = 0;
+    for (int c = 0; c < kClasses; ++c) {
+      from[c] = sum;
+      sum += count[c];
+    }
+    *a.split.n_items = sum;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    const int32_t item = j * kListThreads + tid;
+    if (item >= a.split.tiles) continue;
+    const int32_t place = parts[j] > 1 ? atomicAdd(&places, parts[j]) : -1;
+    a.split.cuts[2 * item] = place;
+    a.split.cuts[2 * item + 1] = parts[j];
+    if (!parts[j]) continue;
+    const int32_t first = from[at[j] >> 24] + (at[j] & 0xffffff);
+    for (int k = 0; k < parts[j]; ++k) {
+      const int32_t lo = t[j].lo + k * length[j];
+      a.split.items[first + k] = {t[j].s, t[j].run, t[j].tile, lo, min(t[j].hi, lo + length[j]), parts[j] > 1 ? place + k : -1};
+    }
+  }
+}
+
 uint64_t magic_of(uint32_t d) { return d <= 1 ? 0 : ~uint64_t(0) / d + 1; }  // ceil(2^64 / d)
 
 // Rows of a KV head that one sequence brings, at most.
 int64_t rows_per_head(const AttendArgs &a) { return int64_t(a.max_fresh) * std::min(a.h.group, a.h.n_q); }
-
-constexpr int32_t kTileGroups = 1024;  // workgroups of many rows that fill the chip
-constexpr int32_t kTileLeast = 512;                       // tokens of the shortest chunk of many rows
 
 // The kernel of few rows holds two tiles of 16, one of more than 128 dimensions.
 bool few(const AttendArgs &a) { return rows_per_head(a) <= (a.c.hd <= 128 ? 32 : 16); }
@@ -134,6 +227,7 @@ struct AttendPlan {
   AttendSplit split;
   int64_t workgroups;
   uint64_t bytes;
+  bool cut;  // many rows: tiles may be cut
 };
 
 // Workgroups of few rows that the chip holds at once: one round of long chunks
@@ -161,22 +255,33 @@ AttendPlan plan_few(const AttendArgs &a, char *ws) {
   return p;
 }
 
-// The workspace holds what no call with these bounds exceeds, whatever its window.
+// A call that fits the chip at once with short contexts needs no list, and one
+// of more tiles than a list takes is even enough without.
 AttendPlan plan_tiles(const AttendArgs &a, char *ws) {
   AttendPlan p{};
   AttendSplit &s = p.split;
-  const int64_t full = int64_t(a.max_ctx) + kTileAlign;
-  const int64_t span = a.window > 0 ? std::min<int64_t>(full, int64_t(a.window) + a.max_fresh + kTileAlign) : full;
-  const int64_t base = std::max<int64_t>(1, groups_of(a)), fill = (kTileGroups + base - 1) / base;
-  const int64_t parts = std::min(fill, (span + kTileLeast - 1) / kTileLeast), most = std::min(fill, (full + kTileLeast - 1) / kTileLeast);
-  s.chunk = int32_t(((span + parts - 1) / parts + kTileAlign - 1) / kTileAlign * kTileAlign);
-  s.n_split = int32_t((span + s.chunk - 1) / s.chunk);
-  p.workgroups = base * s.n_split;
-  if (most == 1) return p;
-  const uint64_t rows = uint64_t(a.max_tokens) * a.h.n_q * uint64_t(most);
-  s.part = reinterpret_cast<float *>(ws);
-  s.part_lse = reinterpret_cast<float *>(ws + padded(rows * a.c.hd * 4));
-  p.bytes = padded(rows * a.c.hd * 4) + padded(rows * 4);
+  p.workgroups = groups_of(a);
+  const int64_t fits = a.c.hd > 128 ? 256 : 512;
+  if (p.workgroups > kListTiles || (p.workgroups <= fits && a.max_ctx <= kTileLeast)) return p;
+  s.tiles = int32_t(p.workgroups);
+  // cut where some of a step's tiles may be longer than the chip's share
+  const int64_t each = (int64_t(a.max_ctx) + kTileAlign + kTileLeast - 1) / kTileLeast;  // parts of a tile, at most
+  p.cut = p.workgroups < 3 * fits && each > 1;
+  const int64_t places = p.cut ? std::min<int64_t>(2 * kTileParts, p.workgroups * each) : 0;
+  if (p.cut) p.workgroups += std::min<int64_t>(kTileParts, p.workgroups * each);
+  const uint64_t rows = uint64_t(places) * kTileRows;
+  uint64_t at = 0;
+  auto take = [&](uint64_t bytes) {
+    char *q = ws + at;
+    at += padded(bytes);
+    return q;
+  };
+  s.n_items = reinterpret_cast<int32_t *>(take(4));
+  s.items = reinterpret_cast<TileItem *>(take(uint64_t(p.workgroups) * sizeof(TileItem)));
+  s.cuts = reinterpret_cast<int32_t *>(take(uint64_t(s.tiles) * 8));
+  s.part = reinterpret_cast<float *>(take(rows * a.c.hd * 4));
+  s.part_lse = reinterpret_cast<float *>(take(rows * 4));
+  p.bytes = at;
   return p;
 }
 
@@ -201,26 +306,35 @@ void attend_launch(const AttendArgs &args, void *ws, void *stream) {
   a.split = p.split;
   a.bt_magic = magic_of(uint32_t(a.c.bt));
   const dim3 work = grid_of(p.workgroups, 256);
-  const bool joined = few(a) ? a.split.n_split > 0 : a.split.n_split > 1;
-  const int64_t rows_each = few(a) ? int64_t(a.n_seq) * a.max_fresh : a.max_tokens;
-  const dim3 rows = joined ? grid_of(rows_each * a.h.n_q, kJoinThreads) : dim3(1);
+  const bool joined = few(a) ? a.split.n_split > 0 : p.cut;
+  const int64_t join_groups = few(a) ? int64_t(a.n_seq) * a.max_fresh * a.h.n_q : int64_t(a.split.tiles) * (kTileRows / kJoinRows);
+  const dim3 rows = joined ? grid_of(join_groups, kJoinThreads) : dim3(1);
   const hipStream_t st = kv_stream(stream);
-  if (few(a))
+  const int32_t lanes = a.c.hd <= 64 ? 16 : a.c.hd <= 128 ? 32 : 64;
+  const bool b = a.dtype == ATP_BF16;
+  if (few(a)) {
     attend_few(a, work, st);
-  else
-    attend_tiles(a, work, st);
-  kv_hip(hipGetLastError(), "atp_kv_attend");
-  if (joined) {
-    const int32_t lanes = a.c.hd <= 64 ? 16 : a.c.hd <= 128 ? 32 : 64;
-    // chunks of a sequence, about
-    const int64_t chunks = few(a) ? a.split.groups / groups_of(a) : a.split.n_split;
-    const dim3 block(chunks > 64 / lanes * 4 ? kJoinThreads : 64);
-    if (a.dtype == ATP_BF16)
-      hipLaunchKernelGGL((k_join<__bf16>), rows, block, 0, st, a, lanes, few(a));
-    else
-      hipLaunchKernelGGL((k_join<_Float16>), rows, block, 0, st, a, lanes, few(a));
     kv_hip(hipGetLastError(), "atp_kv_attend");
+    if (!joined) return;
+    const dim3 block(a.split.groups / groups_of(a) > 64 / lanes * 4 ? kJoinThreads : 64);  // by a sequence's chunks, about
+    if (b)
+      hipLaunchKernelGGL((k_join<__bf16>), rows, block, 0, st, a, lanes);
+    else
+      hipLaunchKernelGGL((k_join<_Float16>), rows, block, 0, st, a, lanes);
+  } else {
+    if (a.split.tiles) {
+      hipLaunchKernelGGL(k_list_tiles, dim3(1), dim3(kListThreads), 0, st, a, p.cut);
+      kv_hip(hipGetLastError(), "atp_kv_attend");
+    }
+    attend_tiles(a, work, st);
+    kv_hip(hipGetLastError(), "atp_kv_attend");
+    if (!joined) return;
+    if (b)
+      hipLaunchKernelGGL((k_join_tiles<__bf16>), rows, dim3(kJoinThreads), 0, st, a, lanes);
+    else
+      hipLaunchKernelGGL((k_join_tiles<_Float16>), rows, dim3(kJoinThreads), 0, st, a, lanes);
   }
+  kv_hip(hipGetLastError(), "atp_kv_attend");
 }
 
 }  // namespace atp

@@ -53,40 +53,24 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
   __shared__ uint8_t there[2][kTileTokens];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
-  const int32_t items = gridDim.x / a.split.n_split, split = blockIdx.x / items, item = blockIdx.x % items;
-  // Run by run, so that neighbours, which go to different dies, have alike work;
-  // in a run the last slots begin first: they see the most tokens.
-  int32_t run = 0, slot = item, h0;
-  int32_t n_slots = int32_t(tile_slots(a, run_heads(a.h, 0, &h0)));
-  if (item >= n_slots) {
-    const int32_t each = int32_t(tile_slots(a, a.h.group)), past = item - n_slots;
-    run = min(1 + past / each, a.h.n_run - 1);
-    slot = past - (run - 1) * each;
-    n_slots = int32_t(tile_slots(a, run_heads(a.h, run, &h0)));
+  TileItem it;
+  if (a.split.items) {
+    if (int32_t(blockIdx.x) >= *a.split.n_items) return;
+    it = a.split.items[blockIdx.x];
+  } else {
+    if (int32_t(blockIdx.x) < a.n_seq && tid == 0 && !sequence(a, blockIdx.x).ok) flag(a.status, ATP_EINVAL);
+    it = tile_of(a, blockIdx.x);
+    if (it.s < 0) return;
   }
-  slot = n_slots - 1 - slot;
-  const int32_t gh = run_heads(a.h, run, &h0);
-  // sequence s has the slots from starts[s] * heads / 128 + s on
-  int32_t s = 0, hi_s = a.n_seq - 1;
-  while (s < hi_s) {
-    const int32_t mid = (s + hi_s + 1) >> 1;
-    if (int64_t(a.starts[mid]) * gh / kTileRows + mid <= slot)
-      s = mid;
-    else
-      hi_s = mid - 1;
-  }
-  if (item < a.n_seq && split == 0 && tid == 0 && !sequence(a, item).ok) flag(a.status, ATP_EINVAL);
+  const int32_t s = __builtin_amdgcn_readfirstlane(it.s), run = __builtin_amdgcn_readfirstlane(it.run), tile = __builtin_amdgcn_readfirstlane(it.tile);
   const Seq q = sequence(a, s);
-  if (!q.ok) return;
-  const int32_t tile = slot - s - int32_t(int64_t(q.r0) * gh / kTileRows), rows = q.n * gh;
-  if (tile < 0 || int64_t(tile) * kTileRows >= rows) return;
+  int32_t h0;
+  const int32_t gh = run_heads(a.h, run, &h0), rows = q.n * gh;
 
   const int32_t kv = a.h.kv0 + run, hd = a.c.hd;
   const int32_t row0 = tile * kTileRows, rowe = min(rows, row0 + kTileRows) - 1;
   const int32_t first_pos = q.cached + row0 / gh, last_pos = q.cached + rowe / gh;  // of the workgroup
-  const int32_t seq_lo = first_seen(a, q.cached, kTileTokens) + split * a.split.chunk;
-  const int32_t lo = max(seq_lo, first_seen(a, first_pos, kTileTokens));
-  const int32_t hi = min(min(q.ctx, seq_lo + a.split.chunk), last_pos + 1);
+  const int32_t lo = __builtin_amdgcn_readfirstlane(it.lo), hi = __builtin_amdgcn_readfirstlane(it.hi);
   const int32_t *const table = a.table + int64_t(s) * a.max_blocks;
   const char *const kbase = a.c.base + int64_t(kv) * a.c.head_stride;
   const float ks = a.c.scales ? a.c.scales[kv] : 1.0f, vs = a.c.scales ? a.c.scales[a.c.n_kv + kv] : 1.0f;
@@ -350,15 +334,16 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
   const float inv = sum == 0 ? 0.0f : vs / sum;
   const float lse2 = sum == 0 ? -INFINITY : top + __builtin_amdgcn_logf(sum);
   const int64_t row = int64_t(q.r0 + tok) * a.h.n_q + head;
-  const bool parts = a.split.n_split > 1;
+  const bool parts = it.place >= 0;
+  const int64_t at_part = int64_t(it.place) * kTileRows + wave * 32 + col;
   if (half == 0) {
     if (parts)
-      a.split.part_lse[row * a.split.n_split + split] = lse2;
+      a.split.part_lse[at_part] = lse2;
     else if (a.lse)
       a.lse[row] = lse2 * kLn2;
   }
   T *const dst = static_cast<T *>(a.out) + (q.r0 + tok) * a.out_stride + int64_t(head) * hd;
-  float *const part = parts ? a.split.part + (row * a.split.n_split + split) * hd : nullptr;
+  float *const part = parts ? a.split.part + at_part * hd : nullptr;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll

@@ -83,14 +83,26 @@ uint64_t attend_workspace(const AttendArgs &a);
 void attend_launch(const AttendArgs &a, void *ws, void *stream);
 
 // How a call's context is cut over workgroups whose results are joined.
-//   many rows  chunk k of every sequence's tokens begins `chunk` tokens behind
-//              chunk k - 1; n_split chunks at most
-//   few rows   the chunks' length is found on the device, for about `groups`
-//              of them over all sequences; workgroup w has the results' place w
+//   few rows   chunks of one length, found on the device, for about `groups`
+//              workgroups over all sequences; workgroup w has the results'
+//              place w, of n_split rows
+//   many rows  a tile of 128 rows and a part of the tokens it sees is an item
+//              of a list made on the device, longest first; each part of a
+//              cut tile has a place of 128 rows.  Without a list, workgroup w
+//              takes the whole tile w.
+struct TileItem {
+  int32_t s, run, tile, lo, hi;  // tokens [lo, hi)
+  int32_t place;                 // of its results; -1: it writes the rows themselves
+  int32_t pad[2];
+};
 struct AttendSplit {
-  int32_t chunk, n_split, groups;
-  float *part, *part_lse;  // [rows][query heads][n_split][dim], [..][n_split] (base 2); few: [w][rows][dim], [w][rows]
+  int32_t groups, n_split;
+  float *part, *part_lse;  // [place][rows][dim], [place][rows] (base 2)
   int32_t *shares;         // few: [n_seq][2], a sequence's first chunk and their number
+  TileItem *items;
+  int32_t *n_items;        // 1 on
+  int32_t *cuts;           // [tiles][2], a tile's first place and the number of its parts (0, 1: not cut)
+  int32_t tiles;
 };
 
 // The checks of the entry points (Error on a refusal), before any HIP call.
