@@ -161,7 +161,7 @@ __device__ inline TileItem tile_of(const AttendArgs &a, int32_t item) {
   const int32_t tile = slot - s - int32_t(int64_t(q.r0) * gh / kTileRows), rows = q.n * gh;
   if (!q.ok || tile < 0 || int64_t(tile) * kTileRows >= rows) return {-1, 0, 0, 0, 0, -1};
   const int32_t row0 = tile * kTileRows, rowe = min(rows, row0 + kTileRows) - 1;
-  return {s, run, tile, first_seen(a, q.cached + row0 / gh, kTileAlign), q.cached + rowe / gh + 1, -1};
+  return {s, run, tile, first_seen(a, q.cached + row0 / gh, kTileAlign), q.cached + rowe / gh + 1, -1, q.r0, q.n, q.cached};
 }
 #endif
 

@@ -90,9 +90,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_tiles(AttendKernel a, int
   const int32_t place = a.split.cuts[2 * item], parts = a.split.cuts[2 * item + 1];
   if (parts <= 1) return;
   const TileItem t = tile_of(a, item);
-  const Seq q = sequence(a, t.s);
   int32_t h0;
-  const int32_t gh = run_heads(a.h, t.run, &h0), rows = q.n * gh, hd = a.c.hd;
+  const int32_t gh = run_heads(a.h, t.run, &h0), rows = t.n * gh, hd = a.c.hd;
   const int at = threadIdx.x % lanes, d = at * 4, each = kJoinThreads / lanes;
   for (int32_t x = threadIdx.x / lanes; x < kJoinRows; x += each) {
     const int32_t in = part * kJoinRows + x, r = t.tile * kTileRows + in;
@@ -124,10 +123,10 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_tiles(AttendKernel a, int
     const float inv = total == 0 ? 0.0f : 1.0f / total;
     const int32_t i = r / gh, h = h0 + r % gh;
     if (d < hd) {
-      T *dst = static_cast<T *>(a.out) + (q.r0 + i) * a.out_stride + int64_t(h) * hd + d;
+      T *dst = static_cast<T *>(a.out) + (t.r0 + i) * a.out_stride + int64_t(h) * hd + d;
       *reinterpret_cast<u32x2_t *>(dst) = u32x2_t{pack2<T>(o[0] * inv, o[1] * inv), pack2<T>(o[2] * inv, o[3] * inv)};
     }
-    if (at == 0 && a.lse) a.lse[int64_t(q.r0 + i) * a.h.n_q + h] = total == 0 ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
+    if (at == 0 && a.lse) a.lse[int64_t(t.r0 + i) * a.h.n_q + h] = total == 0 ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
   }
 }
 
@@ -182,9 +181,10 @@ __global__ void __launch_bounds__(kListThreads) k_list_tiles(AttendKernel a, boo
       from[c] = sum;
       sum += count[c];
     }
-    *a.split.n_items = sum;
+    n = sum;
   }
   __syncthreads();
+  for (int32_t i = n + tid; i < a.split.n_items; i += kListThreads) a.split.items[i].s = -1;
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     const int32_t item = j * kListThreads + tid;
@@ -195,8 +195,11 @@ __global__ void __launch_bounds__(kListThreads) k_list_tiles(AttendKernel a, boo
     if (!parts[j]) continue;
     const int32_t first = from[at[j] >> 24] + (at[j] & 0xffffff);
     for (int k = 0; k < parts[j]; ++k) {
-      const int32_t lo = t[j].lo + k * length[j];
-      a.split.items[first + k] = {t[j].s, t[j].run, t[j].tile, lo, min(t[j].hi, lo + length[j]), parts[j] > 1 ? place + k : -1};
+      TileItem one = t[j];
+      one.lo = t[j].lo + k * length[j];
+      one.hi = min(t[j].hi, one.lo + length[j]);
+      one.place = parts[j] > 1 ? place + k : -1;
+      a.split.items[first + k] = one;
     }
   }
 }
@@ -276,7 +279,7 @@ AttendPlan plan_tiles(const AttendArgs &a, char *ws) {
     at += padded(bytes);
     return q;
   };
-  s.n_items = reinterpret_cast<int32_t *>(take(4));
+  s.n_items = int32_t(p.workgroups);
   s.items = reinterpret_cast<TileItem *>(take(uint64_t(p.workgroups) * sizeof(TileItem)));
   s.cuts = reinterpret_cast<int32_t *>(take(uint64_t(s.tiles) * 8));
   s.part = reinterpret_cast<float *>(take(rows * a.c.hd * 4));

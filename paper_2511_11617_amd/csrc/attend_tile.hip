@@ -51,26 +51,26 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
   constexpr int NCH = kTileTokens * SW::kChunks / kTileThreads;  // chunks a thread stages, of K and of V
   __shared__ __attribute__((aligned(256))) char lds[2][2][kTileTokens * ROW];
   __shared__ uint8_t there[2][kTileTokens];
+  __shared__ int dirty[2];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
   TileItem it;
   if (a.split.items) {
-    if (int32_t(blockIdx.x) >= *a.split.n_items) return;
     it = a.split.items[blockIdx.x];
   } else {
     if (int32_t(blockIdx.x) < a.n_seq && tid == 0 && !sequence(a, blockIdx.x).ok) flag(a.status, ATP_EINVAL);
     it = tile_of(a, blockIdx.x);
-    if (it.s < 0) return;
   }
-  const int32_t s = __builtin_amdgcn_readfirstlane(it.s), run = __builtin_amdgcn_readfirstlane(it.run), tile = __builtin_amdgcn_readfirstlane(it.tile);
-  const Seq q = sequence(a, s);
+  const auto uniform = [](int32_t x) { return __builtin_amdgcn_readfirstlane(x); };
+  const int32_t s = uniform(it.s), run = uniform(it.run), tile = uniform(it.tile), lo = uniform(it.lo), hi = uniform(it.hi);
+  if (s < 0) return;
+  const Seq q = {uniform(it.r0), uniform(it.n), uniform(it.cached), uniform(it.cached) + uniform(it.n), true};
   int32_t h0;
   const int32_t gh = run_heads(a.h, run, &h0), rows = q.n * gh;
 
   const int32_t kv = a.h.kv0 + run, hd = a.c.hd;
   const int32_t row0 = tile * kTileRows, rowe = min(rows, row0 + kTileRows) - 1;
   const int32_t first_pos = q.cached + row0 / gh, last_pos = q.cached + rowe / gh;  // of the workgroup
-  const int32_t lo = __builtin_amdgcn_readfirstlane(it.lo), hi = __builtin_amdgcn_readfirstlane(it.hi);
   const int32_t *const table = a.table + int64_t(s) * a.max_blocks;
   const char *const kbase = a.c.base + int64_t(kv) * a.c.head_stride;
   const float ks = a.c.scales ? a.c.scales[kv] : 1.0f, vs = a.c.scales ? a.c.scales[a.c.n_kv + kv] : 1.0f;
@@ -85,17 +85,6 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
   // the wave's first and last position
   const int32_t wfirst = q.cached + min(row0 + wave * 32, rows - 1) / gh, wlast = q.cached + min(row0 + wave * 32 + 31, rows - 1) / gh;
   const bool idle = row0 + wave * 32 >= rows;  // it only loads
-  v8 qf[KK];
-  {
-    const T *src = static_cast<const T *>(a.q) + (q.r0 + tok) * a.q_stride + int64_t(head) * hd;
-#pragma unroll
-    for (int k = 0; k < KK; ++k) {
-      u32x4_t x = {0, 0, 0, 0};
-      const int d = 16 * k + 8 * half;
-      if (mine && a.scale != 0 && (WHOLE || d < hd)) x = *reinterpret_cast<const u32x4_t *>(src + d) ^ sign;
-      qf[k] = __builtin_bit_cast(v8, x);
-    }
-  }
   float top = -INFINITY, sum = 0;
   f32x16 o[DT];
 #pragma unroll
@@ -176,6 +165,21 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
     }
   };
 
+  // the first tile is on its way while q comes in
+  Regs first_tile;
+  load(lo, 0, first_tile);
+  v8 qf[KK];
+  {
+    const T *src = static_cast<const T *>(a.q) + (q.r0 + tok) * a.q_stride + int64_t(head) * hd;
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+      u32x4_t x = {0, 0, 0, 0};
+      const int d = 16 * k + 8 * half;
+      if (mine && a.scale != 0 && (WHOLE || d < hd)) x = *reinterpret_cast<const u32x4_t *>(src + d) ^ sign;
+      qf[k] = __builtin_bit_cast(v8, x);
+    }
+  }
+
   // Operand A of the second product: of dimension 32 d + lane % 32, the tokens
   // 16 k + 4 half + (0..3) and those 8 further on.
   auto v_operand = [&](const char *vl, int d, int k) __attribute__((always_inline)) {
@@ -215,14 +219,11 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
 #pragma unroll
           for (int e = 0; e < 32; ++e) sc[e / 16][e % 16] = cap2 * tanh_any(sc[e / 16][e % 16] * unit);
         }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) sc[e / 16][e % 16] *= unit;
       }
-      if (a.slopes) {
-        const float from = float(t0 + 4 * half - pos);
+      if (a.slopes) {  // without a cap, the scores have their unit still to come
+        const float from = slope * float(t0 + 4 * half - pos), u = a.softcap > 0 ? 1.0f : unit;
 #pragma unroll
-        for (int e = 0; e < 32; ++e) sc[e / 16][e % 16] = __builtin_fmaf(slope, from + float(token_of(e)), sc[e / 16][e % 16]);
+        for (int e = 0; e < 32; ++e) sc[e / 16][e % 16] = __builtin_fmaf(sc[e / 16][e % 16], u, __builtin_fmaf(slope, float(token_of(e)), from));
       }
     }
     if (mixed) {  // a lane's tokens are t0 + 4 half + token_of(e): seen from the window's begin to its own position
@@ -275,26 +276,36 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
   // unseen, V's values that are not finite become 0, and what of them is seen
   // is added behind the last tile.
   auto clean = [&](int buf) __attribute__((always_inline)) {
-    bool found = false;
-#pragma unroll 1
-    for (int i = tid; i < kTileTokens * ROW / 16; i += kTileThreads) {
-      u32x4_t *const at = reinterpret_cast<u32x4_t *>(&lds[buf][1][i * 16]), x = *at;
-      const bool here = not_finite<T>(x[0]) || not_finite<T>(x[1]) || not_finite<T>(x[2]) || not_finite<T>(x[3]);
-      if (here) *at = u32x4_t{finite_only<T>(x[0]), finite_only<T>(x[1]), finite_only<T>(x[2]), finite_only<T>(x[3])};
-      found |= here;
+    constexpr int kMine = kTileTokens * ROW / 16 / kTileThreads;
+    u32x4_t x[kMine];
+    uint32_t found = 0;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) x[i] = *reinterpret_cast<u32x4_t *>(&lds[buf][1][(i * kTileThreads + tid) * 16]);
+#pragma unroll
+    for (int i = 0; i < kMine; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) found |= not_finite<T>(x[i][j]);
+    if (found) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i)
+        *reinterpret_cast<u32x4_t *>(&lds[buf][1][(i * kTileThreads + tid) * 16]) =
+            u32x4_t{finite_only<T>(x[i][0]), finite_only<T>(x[i][1]), finite_only<T>(x[i][2]), finite_only<T>(x[i][3])};
+      dirty[buf] = 1;
     }
-    return __syncthreads_or(found) != 0;
+    __syncthreads();
+    return dirty[buf] != 0;
   };
 
-  if (lo < hi) {
-    Regs g;
-    load(lo, 0, g);
+  {
+    Regs &g = first_tile;
     store(0, g);
+    if (tid == 0) dirty[0] = 0;
     int buf = 0;
     for (int32_t t0 = lo; t0 < hi; t0 += kTileTokens, buf ^= 1) {
       // this tile has come in for every wave, and none reads the other buffer any more
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
+      if (tid == 0) dirty[buf ^ 1] = 0;  // for the next tile
       const uint64_t seen = __ballot(there[buf][lane] != 0);
       if (t0 + kTileTokens - 1 > first_pos || seen != ~0ull || (a.window > 0 && t0 <= last_pos - a.window)) {
         if (clean(buf)) {

@@ -90,19 +90,19 @@ void attend_launch(const AttendArgs &a, void *ws, void *stream);
 //              of a list made on the device, longest first; each part of a
 //              cut tile has a place of 128 rows.  Without a list, workgroup w
 //              takes the whole tile w.
-struct TileItem {
-  int32_t s, run, tile, lo, hi;  // tokens [lo, hi)
+struct alignas(16) TileItem {
+  int32_t s, run, tile, lo, hi;  // tokens [lo, hi); s < 0: none
   int32_t place;                 // of its results; -1: it writes the rows themselves
-  int32_t pad[2];
+  int32_t r0, n, cached;         // the sequence's first row, new tokens and tokens before
+  int32_t pad[3];
 };
 struct AttendSplit {
   int32_t groups, n_split;
   float *part, *part_lse;  // [place][rows][dim], [place][rows] (base 2)
   int32_t *shares;         // few: [n_seq][2], a sequence's first chunk and their number
   TileItem *items;
-  int32_t *n_items;        // 1 on
   int32_t *cuts;           // [tiles][2], a tile's first place and the number of its parts (0, 1: not cut)
-  int32_t tiles;
+  int32_t tiles, n_items;
 };
 
 // The checks of the entry points (Error on a refusal), before any HIP call.
