@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_tiles(AttendKernel a, int
 // into the list longest first (32 classes of length), so that the last ones to
 // begin are short.
 constexpr int kListThreads = 1024, kListTiles = 4096, kClasses = 32;
-constexpr int32_t kTileParts = 1024, kTileLeast = 512;
+constexpr int32_t kTileParts = 640, kTileLeast = 512;
 __global__ void __launch_bounds__(kListThreads) k_list_tiles(AttendKernel a, bool cut) {
   constexpr int kEach = kListTiles / kListThreads;
   __shared__ int64_t sums[kListThreads / 64];
@@ -269,7 +269,7 @@ AttendPlan plan_tiles(const AttendArgs &a, char *ws) {
   s.tiles = int32_t(p.workgroups);
   // cut where some of a step's tiles may be longer than the chip's share
   const int64_t each = (int64_t(a.max_ctx) + kTileAlign + kTileLeast - 1) / kTileLeast;  // parts of a tile, at most
-  p.cut = p.workgroups < 3 * fits && each > 1;
+  p.cut = p.workgroups < 2 * fits && each > 1;
   const int64_t places = p.cut ? std::min<int64_t>(2 * kTileParts, p.workgroups * each) : 0;
   if (p.cut) p.workgroups += std::min<int64_t>(kTileParts, p.workgroups * each);
   const uint64_t rows = uint64_t(places) * kTileRows;
