@@ -204,6 +204,12 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
   const float ks = a.c.scales ? a.c.scales[kv] : 1.0f, vs = a.c.scales ? a.c.scales[a.c.n_kv + kv] : 1.0f;
   const float unit = a.scale * ks * (a.softcap > 0 ? 1.0f / a.softcap : kLog2e), cap2 = a.softcap * kLog2e;
 
+  // The 8 dimensions that a lane brings to the k-th inner step of the first
+  // product, of K and of q alike; in an 8-bit row, two steps' are side by side,
+  // one 16-byte read.
+  constexpr bool PAIRED = WHOLE && sizeof(CT) == 1;
+  const auto dim_of = [&](int k) { return PAIRED ? 64 * (k / 2) + 16 * grp + 8 * (k % 2) : 32 * k + 8 * grp; };
+
   // rows of this lane: column `col` of each tile
   int32_t pos[MT];
   float slope[MT];
@@ -216,7 +222,7 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
     const T *src = static_cast<const T *>(a.q) + (q.r0 + i) * a.q_stride + int64_t(h) * hd;
 #pragma unroll
     for (int k = 0; k < KK; ++k) {
-      const int d = 32 * k + 8 * grp;
+      const int d = dim_of(k);
       u32x4_t x = {0, 0, 0, 0};
       if (m * 16 + col < rows && (WHOLE || d < hd)) x = *reinterpret_cast<const u32x4_t *>(src + d);
       qf[m][k] = __builtin_bit_cast(v8, x);
@@ -258,8 +264,16 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
         if (p >= 0) x.there |= 0xfu << (4 * u);
         const char *const kt = kbase + off, *const vt = vbase + off;
 #pragma unroll
-        for (int k = 0; k < KK; ++k)
-          x.k[u][k] = *reinterpret_cast<const typename KC::raw *>(kt + uint32_t(col * a.c.tok_stride + (32 * k + 8 * grp) * int(sizeof(CT))));
+        for (int k = 0; k < KK; k += PAIRED ? 2 : 1) {
+          const char *const from = kt + uint32_t(col * a.c.tok_stride + dim_of(k) * int(sizeof(CT)));
+          if constexpr (PAIRED) {
+            const u32x4_t w = *reinterpret_cast<const u32x4_t *>(from);
+            x.k[u][k] = typename KC::raw{w[0], w[1]};
+            x.k[u][k + 1] = typename KC::raw{w[2], w[3]};
+          } else {
+            x.k[u][k] = *reinterpret_cast<const typename KC::raw *>(from);
+          }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -274,8 +288,8 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
 #pragma unroll
         for (int k = 0; k < KK; ++k) {
           x.k[u][k] = typename KC::raw{};
-          if (32 * k + 8 * grp < hd)
-            x.k[u][k] = *reinterpret_cast<const typename KC::raw *>(kbase + off + (32 * k + 8 * grp) * int(sizeof(CT)));
+          if (dim_of(k) < hd)
+            x.k[u][k] = *reinterpret_cast<const typename KC::raw *>(kbase + off + dim_of(k) * int(sizeof(CT)));
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -398,19 +412,20 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
       }
   };
 
-  // the next step's reads are in flight while one is computed
-  int32_t t0 = lo + wave * TS;
-  if (t0 < hi) {
-    Step x;
-    load(t0, x);
-    while (true) {
-      const int32_t t1 = t0 + kFewWaves * TS;
-      Step y;
+  // The next step's reads are in flight while one is computed: two sets of
+  // registers in turn, as moving them would wait for the reads.
+  {
+    Step x, y;
+    int32_t t0 = lo + wave * TS;
+    if (t0 < hi) load(t0, x);
+    while (t0 < hi) {
+      const int32_t t1 = t0 + kFewWaves * TS, t2 = t1 + kFewWaves * TS;
       if (t1 < hi) load(t1, y);
       compute(t0, x);
       if (t1 >= hi) break;
-      x = y;
-      t0 = t1;
+      if (t2 < hi) load(t2, x);
+      compute(t1, y);
+      t0 = t2;
     }
   }
 #pragma unroll 1
