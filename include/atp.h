@@ -650,7 +650,7 @@ int atp_kv_append(const atp_kv_cache *cache, const atp_kv_step *step, int32_t la
 /* What a token of the step sees: of its own sequence the tokens t at or
  * before its position p, with `window` > 0 only those with p - t < window,
  * and none whose block is -1 in the table.  The score of query head h is
- * scale * q.k, then softcap * tanh(score / softcap) if softcap > 0, then
+ * scale * q.k, then softcap * tanh(score / softcap) if softcap > 0 (1e-6 on), then
  * + slopes[h] * (t - p) if slopes is given (device float [query heads]). */
 typedef struct {
   float scale, softcap;

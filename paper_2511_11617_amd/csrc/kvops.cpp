@@ -280,7 +280,7 @@ void kv_attend(const atp_kv_cache *cache, const atp_kv_step *step, int32_t layer
   a.c = check_arena(*cache, layer);
   want(mask != nullptr, "mask is NULL");
   want(std::isfinite(mask->scale), "mask: scale must be finite");
-  want(std::isfinite(mask->softcap) && mask->softcap >= 0, "mask: softcap must be 0 or positive");
+  want(std::isfinite(mask->softcap) && (mask->softcap == 0 || mask->softcap >= 1e-6f), "mask: softcap must be 0 or at least 1e-6");
   want(mask->window >= 0, "mask: negative window");
   check_words(mask->slopes, 4, "mask: slopes", true);
   check_words(step->status, 4, "step: status", true);

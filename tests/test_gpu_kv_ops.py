@@ -189,6 +189,13 @@ ATTEND = {
     "prompt_e4m3_fp16": dict(cached=[100, 0], fresh=[60, 90], cache="e4m3", dtype="fp16", hd=64, layout="token", **GQA),
     "chunk_behind_much": dict(cached=[6000], fresh=[40], q_heads=(0, 4), group=4),
     "two_layers": dict(cached=[40, 9], fresh=[1, 20], layers=3, **GQA),
+    "mixed_batch": dict(cached=[0, 3000] + [20 * i for i in range(38)], fresh=[300, 1] + [1] * 30 + [0, 2] * 4, pad=7, **GQA),
+    "prompt_behind_fp16_token": dict(cached=[2000, 31], fresh=[50, 70], dtype="fp16", layout="token", bt=32, **GQA),
+    "prompt_of_one_head": dict(cached=[100], fresh=[300], q_heads=(2, 3), kv_heads=(1, 2), group=2),
+    "many_sequences": dict(cached=[(37 * i) % 90 for i in range(600)], fresh=[1] * 600, q_heads=(0, 2), group=2, hd=64),
+    "many_sequences_some_long": dict(cached=[(37 * i) % 90 + 1500 * (i % 97 == 5) for i in range(300)], fresh=[1 - (i % 11 == 3) for i in range(300)],
+                                     q_heads=(1, 4), kv_heads=(0, 2), group=2, hd=64, layout="token"),
+    "more_tiles_than_a_list": dict(cached=[i % 7 for i in range(4100)], fresh=[40] + [1] * 4099, q_heads=(0, 1), group=1, hd=64),
     "loose_bounds": dict(cached=[500, 77], fresh=[1, 2], bounds=(64, 5000), **GQA),
     "loose_bounds_one": dict(cached=[500, 77], fresh=[1, 1], bounds=(1, 40000), **GQA),
 }
@@ -212,10 +219,10 @@ MASKS = {
 
 
 @pytest.mark.parametrize("mask", MASKS)
-@pytest.mark.parametrize("shape", ["decode", "drafts", "prompt", "long"])
+@pytest.mark.parametrize("shape", ["decode", "drafts", "prompt", "long", "behind"])
 def test_attend_masks(shape, mask):
     kw = {"decode": dict(cached=[300, 40, 0], fresh=[1, 1, 1]), "drafts": dict(cached=[200, 31], fresh=[4, 2], dtype="fp16"),
-          "prompt": dict(cached=[70, 0], fresh=[90, 140]), "long": dict(cached=[5000, 3100], fresh=[1, 1], layout="token")}[shape]
+          "prompt": dict(cached=[70, 0], fresh=[90, 140]), "behind": dict(cached=[1700, 40], fresh=[40, 9], dtype="fp16"), "long": dict(cached=[5000, 3100], fresh=[1, 1], layout="token")}[shape]
     s = Setup(**kw, **GQA, seed=3)
     m = dict(MASKS[mask])
     if m.get("slopes"):

@@ -196,10 +196,15 @@ def test_row_refusals():
 
 def test_attend_mask_and_bound_refusals():
     _refused(atp.EINVAL, "scale", _attend, mask=atp.Mask(math.nan))
-    _refused(atp.EINVAL, "softcap", _attend, mask=atp.Mask(1.0, softcap=-1.0))
+    for cap in (-1.0, 1e-7, math.inf, math.nan):
+        _refused(atp.EINVAL, "softcap", _attend, mask=atp.Mask(1.0, softcap=cap))
     _refused(atp.EINVAL, "window", _attend, mask=atp.Mask(1.0, window=-1))
     _refused(atp.EINVAL, "max_ctx", _attend, s=_step(max_ctx=1))
     _refused(atp.EINVAL, "negative bound", _attend, s=_step(max_fresh=-1))
+    _refused(atp.EINVAL, "2^30", _attend, s=_step(max_ctx=(1 << 30) + 1))
+    _refused(atp.EINVAL, "int32", _attend, s=_step(max_tokens=1 << 29))
+    # HIP counts a launch's threads in 32 bits
+    _refused(atp.EINVAL, "one launch", _attend, s=_step(n_seq=1 << 23, max_blocks=1, max_fresh=1, max_ctx=16, max_tokens=8))
 
 
 def test_attend_workspace_refusals():
