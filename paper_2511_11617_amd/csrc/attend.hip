@@ -82,8 +82,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(AttendKernel a, int32_t l
   if (tid == 0 && a.lse) a.lse[row] = total == 0 ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
-// Many rows: a workgroup takes 16 rows of a cut tile; `lanes` lanes a row.
-constexpr int kJoinRows = 16;
+// Many rows: a workgroup takes 4 rows of a cut tile, `lanes` lanes each (a tile
+// cut into hundreds of parts needs many workgroups on them).
+constexpr int kJoinRows = 4;
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) k_join_tiles(AttendKernel a, int32_t lanes) {
   const int32_t item = blockIdx.x / (kTileRows / kJoinRows), part = blockIdx.x % (kTileRows / kJoinRows);
@@ -92,10 +93,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_tiles(AttendKernel a, int
   const TileItem t = tile_of(a, item);
   int32_t h0;
   const int32_t gh = run_heads(a.h, t.run, &h0), rows = t.n * gh, hd = a.c.hd;
-  const int at = threadIdx.x % lanes, d = at * 4, each = kJoinThreads / lanes;
-  for (int32_t x = threadIdx.x / lanes; x < kJoinRows; x += each) {
-    const int32_t in = part * kJoinRows + x, r = t.tile * kTileRows + in;
-    if (r >= rows) break;
+  const int at = threadIdx.x % lanes, d = at * 4;
+  const int32_t in = part * kJoinRows + threadIdx.x / lanes, r = t.tile * kTileRows + in;
+  if (r < rows) {
     const float *lse = a.split.part_lse + int64_t(place) * kTileRows + in;
     float most = -INFINITY, total = 0;
     for (int c = at; c < parts; c += lanes) most = fmaxf(most, lse[int64_t(c) * kTileRows]);
@@ -333,9 +333,9 @@ void attend_launch(const AttendArgs &args, void *ws, void *stream) {
     kv_hip(hipGetLastError(), "atp_kv_attend");
     if (!joined) return;
     if (b)
-      hipLaunchKernelGGL((k_join_tiles<__bf16>), rows, dim3(kJoinThreads), 0, st, a, lanes);
+      hipLaunchKernelGGL((k_join_tiles<__bf16>), rows, dim3(kJoinRows * lanes), 0, st, a, lanes);
     else
-      hipLaunchKernelGGL((k_join_tiles<_Float16>), rows, dim3(kJoinThreads), 0, st, a, lanes);
+      hipLaunchKernelGGL((k_join_tiles<_Float16>), rows, dim3(kJoinRows * lanes), 0, st, a, lanes);
   }
   kv_hip(hipGetLastError(), "atp_kv_attend");
 }

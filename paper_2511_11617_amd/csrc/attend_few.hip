@@ -179,10 +179,16 @@ __device__ inline Share share_of(const AttendKernel &a) {
           __builtin_amdgcn_readfirstlane(mine[3])};
 }
 
-// HD: dimensions the registers hold (head_dim is at most HD); WHOLE: head_dim
-// is HD and block_tokens a multiple of 16, so that a tile of 16 tokens lies
-// in one block and its id is the wave's (scalar); MT: tiles of 16 rows.
-template <typename T, typename CT, int HD, bool WHOLE, int MT>
+// HD: dimensions the registers hold (head_dim is at most HD).  How rows lie:
+//   WHOLE   head_dim is HD and block_tokens a multiple of 16, so that a tile of
+//           16 tokens lies in one block and its id is the wave's (scalar)
+//   EVEN    block_tokens a multiple of 16
+//   ANY     each lane looks its tokens' blocks up
+// Where head_dim is less than HD, dimensions beyond it are read from the row's
+// begin; K's are made 0, V's end in results that nobody takes.
+// MT: tiles of 16 rows.
+enum { WHOLE = 0, EVEN = 1, ANY = 2 };
+template <typename T, typename CT, int HD, int LIE, int MT>
 __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT == 2) ? 1 : 2) k_few(AttendKernel a) {
   using H = Half16<T>;
   using v8 = typename H::v8;
@@ -207,7 +213,7 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
   // The 8 dimensions that a lane brings to the k-th inner step of the first
   // product, of K and of q alike; in an 8-bit row, two steps' are side by side,
   // one 16-byte read.
-  constexpr bool PAIRED = WHOLE && sizeof(CT) == 1;
+  constexpr bool PAIRED = LIE == WHOLE && sizeof(CT) == 1;
   const auto dim_of = [&](int k) { return PAIRED ? 64 * (k / 2) + 16 * grp + 8 * (k % 2) : 32 * k + 8 * grp; };
 
   // rows of this lane: column `col` of each tile
@@ -224,7 +230,7 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
     for (int k = 0; k < KK; ++k) {
       const int d = dim_of(k);
       u32x4_t x = {0, 0, 0, 0};
-      if (m * 16 + col < rows && (WHOLE || d < hd)) x = *reinterpret_cast<const u32x4_t *>(src + d);
+      if (m * 16 + col < rows && (LIE == WHOLE || d < hd)) x = *reinterpret_cast<const u32x4_t *>(src + d);
       qf[m][k] = __builtin_bit_cast(v8, x);
     }
   }
@@ -245,6 +251,8 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
     typename VC::raw v[U][4][VP];
     uint32_t there;
   };
+  const bool quads = a.c.bt % 4 == 0;  // 4 tokens from a multiple of 4 on lie in one block
+  const int32_t row_step = a.c.tok_stride;
   int32_t left_lo = INT32_MAX, left_hi = 0;  // the wave's steps with infinities or NaN still to be added
   bool bad = false;
   auto block_of = [&](int32_t t) __attribute__((always_inline)) -> int32_t {  // t's block id, -1 for none
@@ -253,55 +261,56 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
     if (p < -1 || p >= a.c.num_blocks) bad = true;
     return uint32_t(p) < uint32_t(a.c.num_blocks) ? p : -1;
   };
+  // bytes of a lane's chunks in a row; beyond head_dim: the row's begin
+  uint32_t kd[KK], vd[VP];
+#pragma unroll
+  for (int k = 0; k < KK; ++k) kd[k] = (LIE == WHOLE || dim_of(k) < hd ? dim_of(k) : 0) * int(sizeof(CT));
+#pragma unroll
+  for (int c = 0; c < VP; ++c) vd[c] = (LIE == WHOLE || col * ND + c * NV < hd ? col * ND + c * NV : 0) * int(sizeof(CT));
+  auto offset_of = [&](int32_t t, int32_t p) __attribute__((always_inline)) -> int64_t {  // of token t's row; an absent one is read from block 0 and masked
+    return p < 0 ? 0 : p * a.c.block_stride + int64_t(t - int32_t(divided(t, a.bt_magic)) * a.c.bt) * a.c.tok_stride;
+  };
   auto load = [&](int32_t t0, Step &x) __attribute__((always_inline)) {
     x.there = 0;
-    if constexpr (WHOLE) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < U; ++u) {
+      const char *kt, *vt;  // of the lane's token of K, of its first of V
+      if constexpr (LIE != ANY) {
         const int32_t t = t0 + 16 * u, p = block_of(t);
-        // an absent tile is read from block 0 and masked
-        const int64_t off = p < 0 ? 0 : p * a.c.block_stride + int64_t(t - int32_t(divided(t, a.bt_magic)) * a.c.bt) * a.c.tok_stride;
+        const int64_t off = offset_of(t, p);
         if (p >= 0) x.there |= 0xfu << (4 * u);
-        const char *const kt = kbase + off, *const vt = vbase + off;
+        kt = kbase + off + uint32_t(col * a.c.tok_stride);
+        vt = vbase + off + uint32_t(4 * grp * a.c.tok_stride);
+      } else {
+        const int32_t t = t0 + 16 * u + col, tv = t0 + 16 * u + 4 * grp;
+        kt = kbase + offset_of(t, block_of(t));
+        const int32_t p = block_of(tv);
+        vt = vbase + offset_of(tv, p);
+        if (quads && p >= 0) x.there |= 0xfu << (4 * u);
+      }
 #pragma unroll
-        for (int k = 0; k < KK; k += PAIRED ? 2 : 1) {
-          const char *const from = kt + uint32_t(col * a.c.tok_stride + dim_of(k) * int(sizeof(CT)));
-          if constexpr (PAIRED) {
-            const u32x4_t w = *reinterpret_cast<const u32x4_t *>(from);
-            x.k[u][k] = typename KC::raw{w[0], w[1]};
-            x.k[u][k + 1] = typename KC::raw{w[2], w[3]};
-          } else {
-            x.k[u][k] = *reinterpret_cast<const typename KC::raw *>(from);
-          }
+      for (int k = 0; k < KK; k += PAIRED ? 2 : 1) {
+        if constexpr (PAIRED) {
+          const u32x4_t w = *reinterpret_cast<const u32x4_t *>(kt + kd[k]);
+          x.k[u][k] = typename KC::raw{w[0], w[1]};
+          x.k[u][k + 1] = typename KC::raw{w[2], w[3]};
+        } else {
+          x.k[u][k] = *reinterpret_cast<const typename KC::raw *>(kt + kd[k]);
         }
+      }
+      if (LIE != ANY || quads) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int c = 0; c < VP; ++c)
-            x.v[u][i][c] = *reinterpret_cast<const typename VC::raw *>(vt + uint32_t((4 * grp + i) * a.c.tok_stride + (col * ND + c * NV) * int(sizeof(CT))));
-      }
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int32_t tk = t0 + 16 * u + col, pk = block_of(tk);
-        const int64_t off = pk < 0 ? 0 : pk * a.c.block_stride + int64_t(tk - int32_t(divided(tk, a.bt_magic)) * a.c.bt) * a.c.tok_stride;
-#pragma unroll
-        for (int k = 0; k < KK; ++k) {
-          x.k[u][k] = typename KC::raw{};
-          if (dim_of(k) < hd)
-            x.k[u][k] = *reinterpret_cast<const typename KC::raw *>(kbase + off + dim_of(k) * int(sizeof(CT)));
-        }
+            x.v[u][i][c] = *reinterpret_cast<const typename VC::raw *>(vt + uint32_t(i * row_step) + vd[c]);
+      } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int32_t t = t0 + 16 * u + 4 * grp + i, p = block_of(t);
-          const int64_t vo = p < 0 ? 0 : p * a.c.block_stride + int64_t(t - int32_t(divided(t, a.bt_magic)) * a.c.bt) * a.c.tok_stride;
           if (p >= 0) x.there |= 1u << (4 * u + i);
 #pragma unroll
-          for (int c = 0; c < VP; ++c) {
-            x.v[u][i][c] = typename VC::raw{};
-            if (col * ND + c * NV < hd)
-              x.v[u][i][c] = *reinterpret_cast<const typename VC::raw *>(vbase + vo + (col * ND + c * NV) * int(sizeof(CT)));
-          }
+          for (int c = 0; c < VP; ++c) x.v[u][i][c] = *reinterpret_cast<const typename VC::raw *>(vbase + offset_of(t, p) + vd[c]);
         }
       }
     }
@@ -334,7 +343,11 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
       for (int u = 0; u < U; ++u) {
         sc[u] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < KK; ++k) sc[u] = H::mfma16(KC::operand(x.k[u][k]), qf[m][k], sc[u]);
+        for (int k = 0; k < KK; ++k) {
+          typename KC::raw kx = x.k[u][k];
+          if (LIE != WHOLE && dim_of(k) >= hd) kx = typename KC::raw{};
+          sc[u] = H::mfma16(KC::operand(kx), qf[m][k], sc[u]);
+        }
       }
       // the lane's tokens are t0 + 4 grp + token_of(e)
       float z[4 * U];
@@ -443,7 +456,7 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
 #pragma unroll
           for (int e = 0; e < ND; ++e) {
             const int d = (4 * grp + i) * ND + e;
-            const float y = WHOLE || d < hd ? as_f32(v[d]) : 0.0f;
+            const float y = LIE == WHOLE || d < hd ? as_f32(v[d]) : 0.0f;
             o[m][e][i] += fabsf(y) <= FLT_MAX ? 0.0f : y;
           }
       }
@@ -487,7 +500,7 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
       const int64_t row = int64_t(q.r0 + i) * a.h.n_q + h;
 #pragma unroll
       for (int d = part * 4; d < HD; d += 64) {
-        if (!WHOLE && d >= hd) break;
+        if (LIE != WHOLE && d >= hd) break;
         f32x4 x = {0, 0, 0, 0};
 #pragma unroll
         for (int w = 0; w < kFewWaves; ++w) x += *reinterpret_cast<const f32x4 *>(&so[w][r][d]) * f[w];
@@ -509,35 +522,37 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
   }
 }
 
-template <typename T, typename CT, int HD, bool WHOLE>
+template <typename T, typename CT, int HD, int LIE>
 void launch(const AttendKernel &a, dim3 grid, hipStream_t st) {
   const dim3 block(kFewWaves * 64);
   const int64_t rows = int64_t(a.max_fresh) * std::min(a.h.group, a.h.n_q);
   if constexpr (HD <= 128) {  // two tiles of 256 dimensions do not fit the registers
     if (rows > 16) {
-      hipLaunchKernelGGL((k_few<T, CT, HD, WHOLE, 2>), grid, block, 0, st, a);
+      hipLaunchKernelGGL((k_few<T, CT, HD, LIE, 2>), grid, block, 0, st, a);
       return;
     }
   }
-  hipLaunchKernelGGL((k_few<T, CT, HD, WHOLE, 1>), grid, block, 0, st, a);
+  hipLaunchKernelGGL((k_few<T, CT, HD, LIE, 1>), grid, block, 0, st, a);
+}
+
+template <typename T, typename CT, int HD>
+void by_rows(const AttendKernel &a, dim3 grid, hipStream_t st) {
+  if (a.c.bt % 16)
+    launch<T, CT, HD, ANY>(a, grid, st);
+  else if (a.c.hd < HD)
+    launch<T, CT, HD, EVEN>(a, grid, st);
+  else
+    launch<T, CT, HD, WHOLE>(a, grid, st);
 }
 
 template <typename T, typename CT>
 void by_shape(const AttendKernel &a, dim3 grid, hipStream_t st) {
-  const int hd = a.c.hd;
-  const bool even = a.c.bt % 16 == 0;
-  if (hd == 64 && even)
-    launch<T, CT, 64, true>(a, grid, st);
-  else if (hd == 128 && even)
-    launch<T, CT, 128, true>(a, grid, st);
-  else if (hd == 256 && even)
-    launch<T, CT, 256, true>(a, grid, st);
-  else if (hd <= 64)
-    launch<T, CT, 64, false>(a, grid, st);
-  else if (hd <= 128)
-    launch<T, CT, 128, false>(a, grid, st);
+  if (a.c.hd <= 64)
+    by_rows<T, CT, 64>(a, grid, st);
+  else if (a.c.hd <= 128)
+    by_rows<T, CT, 128>(a, grid, st);
   else
-    launch<T, CT, 256, false>(a, grid, st);
+    by_rows<T, CT, 256>(a, grid, st);
 }
 
 }  // namespace
