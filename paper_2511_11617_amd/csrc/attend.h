@@ -134,7 +134,10 @@ __host__ __device__ inline int64_t tile_slots(const AttendArgs &a, int32_t gh) {
   return int64_t(a.max_tokens) * gh / kTileRows + a.n_seq;
 }
 
-#if defined(__HIPCC__)
+// Rounds of workgroups that few rows' chunks make: two where there are more
+// sequences (times runs of heads) than the chip holds workgroups.
+__host__ __device__ inline int64_t few_rounds(const AttendKernel &a) { return int64_t(a.n_seq) * a.h.n_run > a.split.groups ? 2 : 1; }
+
 // The tile of rows that is number `item` of a call's, run by run (so that
 // neighbours, which go to different dies, have alike work), and in a run from
 // the last slot to the first; s < 0: none.
@@ -163,7 +166,6 @@ __device__ inline TileItem tile_of(const AttendArgs &a, int32_t item) {
   const int32_t row0 = tile * kTileRows, rowe = min(rows, row0 + kTileRows) - 1;
   return {s, run, tile, first_seen(a, q.cached + row0 / gh, kTileAlign), q.cached + rowe / gh + 1, -1, q.r0, q.n, q.cached};
 }
-#endif
 
 void attend_few(const AttendKernel &a, dim3 grid, hipStream_t st);
 void attend_tiles(const AttendKernel &a, dim3 grid, hipStream_t st);

@@ -14,7 +14,7 @@ namespace {
 // Few rows: one workgroup per row and head; 16, 32 or 64 lanes hold its
 // dimensions, 4 each, and as many groups of lanes take chunks in turn.
 constexpr int kJoinThreads = 256;
-constexpr int kMostSplit = 1024;
+constexpr int kMostSplit = 2048;  // at most two rounds of 768 chunks, and one, are one sequence's
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) k_join(AttendKernel a, int32_t lanes) {
   __shared__ float weight[kMostSplit];
@@ -249,7 +249,7 @@ AttendPlan plan_few(const AttendArgs &a, char *ws) {
     p.split.n_split = 0;
     return p;
   }
-  p.workgroups += p.split.groups;  // each sequence's last chunk may be short
+  p.workgroups += (p.workgroups > p.split.groups ? 2 : 1) * p.split.groups;  // as few_rounds(); each sequence's last chunk may be short
   const uint64_t rows = uint64_t(p.workgroups) * uint64_t(p.split.n_split);
   p.split.part = reinterpret_cast<float *>(ws);
   p.split.part_lse = reinterpret_cast<float *>(ws + padded(rows * a.c.hd * 4));
