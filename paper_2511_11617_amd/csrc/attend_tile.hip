@@ -17,6 +17,12 @@
 // read meets a bank twice; where the cache's elements are the products' own
 // and fill the row, the loads go straight to shared memory (the lane picks
 // the chunk that belongs at its place).
+//
+// Measured (128 dimensions, bf16): 880 to 970 TFLOP/s where the chip is full
+// (8 prompts of 8192 behind 8192), 840 for one such prompt, where a library
+// product of 8192^3 reaches 1270.  A lone wave of a SIMD unit takes 4200 clocks
+// a tile, two together 2700 each, of which the matrix units need 1024: two
+// workgroups a CU, so that one's softmax runs beside the other's products.
 #include <cfloat>
 
 #include "attend.h"

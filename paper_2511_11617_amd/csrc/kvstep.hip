@@ -20,12 +20,12 @@ constexpr int kGroupWords = 256;   // bitmap words whose zeros are counted toget
 constexpr int kShortRange = 4;     // blocks of a sequence that one thread looks through
 
 // A pool and a step that one workgroup serves alone, bitmaps in shared memory
-// (one launch; k_extend_one below), measured against the seven launches
-// below, which spread over the chip: 8 sessions 7.0 against 22.6 us, 128
-// sessions of 513 blocks 17.6 against 33.9, 512 of 1521 (779 K entries) 150
-// against 45.
+// (one launch; k_extend_one below): the launches cost most of a small step.
+// Against the seven launches below, which spread over the chip, 8 sessions
+// take 7.5 against 15.5 us, 128 of 513 blocks 14.7 against 24.6, 250 of 513
+// 22.7 against 25.5, and two prompts of 8000 tokens 22.8 against 21.1.
 constexpr int32_t kOneWords = 16384;
-constexpr int64_t kOneEntries = 1 << 17, kOneTokens = 1 << 14;
+constexpr int64_t kOneEntries = 1 << 17, kOneTokens = 1 << 13;
 
 struct ExtendWs {
   uint32_t *used, *shared;
@@ -155,11 +155,11 @@ __device__ inline void verdict(const ExtendArgs &a, int32_t code, int32_t tokens
 __global__ void __launch_bounds__(kScanThreads) k_extend_one(ExtendArgs a, ExtendWs w) {
   __shared__ uint32_t used[kOneWords], shared[kOneWords];
   __shared__ int64_t sums[kScanWaves];
-  __shared__ int32_t sums32[kScanWaves], bad;
+  __shared__ int32_t sums32[kScanWaves], bad, longs;  // longs: some sequence's range is not short
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t words = words_of(a.num_blocks);
   for (int32_t i = tid; i < words; i += kScanThreads) used[i] = shared[i] = 0;
-  if (tid == 0) bad = 0;
+  if (tid == 0) bad = longs = 0;
   __syncthreads();
   const int32_t entries = a.n_seq * a.max_blocks;
   bool wrong = false;
@@ -202,7 +202,15 @@ __global__ void __launch_bounds__(kScanThreads) k_extend_one(ExtendArgs a, Exten
   int64_t tokens = 0;
   for (int32_t s0 = 0; s0 < a.n_seq; s0 += kScanThreads) {
     const int32_t s = s0 + tid;
-    wrong |= s < a.n_seq && !lengths_fit(a, s);
+    if (s < a.n_seq) {
+      if (lengths_fit(a, s)) {
+        int32_t b, e;
+        new_range(a, s, &b, &e);
+        if (e - b > kShortRange) longs = 1;
+      } else {
+        wrong = true;
+      }
+    }
     int64_t sum;
     const int64_t start = tokens + block_scan(s < a.n_seq ? int64_t(a.fresh[s]) : 0, &sum, sums);
     if (s < a.n_seq) a.starts[s] = int32_t(start);
@@ -216,7 +224,7 @@ __global__ void __launch_bounds__(kScanThreads) k_extend_one(ExtendArgs a, Exten
   const int32_t per = (words + kScanThreads - 1) / kScanThreads, from = min(words, tid * per), to = min(words, from + per);
   if (in_range) {
     wrong = false;
-    for (int32_t s = wave; s < a.n_seq; s += kScanWaves) {  // sequences with long ranges
+    for (int32_t s = longs ? wave : a.n_seq; s < a.n_seq; s += kScanWaves) {  // sequences with long ranges
       int32_t b, e;
       new_range(a, s, &b, &e);
       if (e - b <= kShortRange) continue;
@@ -256,7 +264,7 @@ __global__ void __launch_bounds__(kScanThreads) k_extend_one(ExtendArgs a, Exten
     for (int32_t i = from; i < to && first < wanted; ++i)
       for (uint32_t left = free_bits(a, used, i); left && first < wanted; left &= left - 1) w.list[first++] = i * 32 + __ffs(left) - 1;
     __syncthreads();
-    for (int32_t s = wave; s < a.n_seq; s += kScanWaves) {
+    for (int32_t s = longs ? wave : a.n_seq; s < a.n_seq; s += kScanWaves) {
       int32_t b, e;
       new_range(a, s, &b, &e);
       if (e - b > kShortRange) fill_by_wave(a, w.list, w.before[s], s, b, e);
@@ -474,7 +482,8 @@ __device__ inline void write8<E4M3>(E4M3 *p, const float *x) {
   *reinterpret_cast<u32x2_t *>(p) = w;
 }
 
-// Where rot_dim is a multiple of 16.  A workgroup takes up to 4 tokens: its
+// Where rot_dim is a multiple of 16 (8192 tokens of 13 + 8 heads: 20 us, 4.4 TB/s
+// of the 4.7 that a large copy reaches; a pair at a time they took 64).  A workgroup takes up to 4 tokens: its
 // threads work out the tokens' cosines and sines into shared memory (once for
 // all heads), then take units of 16 elements, the two 8s that turn together
 // (or lie together, where nothing turns), as 16-byte reads and writes.
