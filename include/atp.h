@@ -10,6 +10,8 @@
  *                        new shard layout and land the missing bytes
  *   atp_reshard_kv       the same for the paged KV cache (block ids kept)
  *   atp_sync             wait for both, report the first asynchronous error
+ * and what a serving step does on the cache between two of them:
+ *   atp_kv_extend, atp_kv_append, atp_kv_attend
  *
  * Conventions
  *   - Status: every int-returning call returns ATP_OK (0) or a negative
@@ -22,8 +24,8 @@
  *     freed with atp_plan_free.
  *   - Streams: atp_stream is a hipStream_t.  Calls only enqueue work and
  *     return; atp_sync blocks.
- *   - Bytes are copied, never converted: any 16-bit payload (NaN, -0,
- *     denormals) arrives unchanged.
+ *   - The reshard copies bytes and never converts: any 16-bit payload (NaN,
+ *     -0, denormals) arrives unchanged.
  *   - Threading: a plan is used by one host thread at a time.  Several
  *     plans may be pending on one device at once, each on buffers of its
  *     own; those issued on the same (compute, copy) pair run their side
