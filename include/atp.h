@@ -46,7 +46,8 @@ enum {
   ATP_EINVAL = -1,    /* malformed problem, bad argument, bad block table  */
   ATP_ECAPACITY = -2, /* an arena, staging or host buffer is too small     */
   ATP_EHIP = -3,      /* a HIP runtime call failed                         */
-  ATP_EALIGN = -4,    /* a device buffer is not 256-byte aligned           */
+  ATP_EALIGN = -4,    /* a device buffer is not aligned (256 bytes, unless */
+                      /* its call says otherwise)                          */
   ATP_ESTATE = -5     /* call out of order (reshard again before atp_sync) */
 };
 
@@ -584,7 +585,7 @@ typedef struct {
   int64_t *slots;        /* device [max_tokens]: block * block_tokens +
                             offset of each token, -1 = padding               */
   int32_t *positions;    /* device [max_tokens]: position in its sequence    */
-  int32_t max_tokens;    /* rows                                             */
+  int32_t max_tokens;    /* rows (atp_kv_append: below 2^26)                 */
   int32_t max_fresh;     /* at least every fresh[s]           (atp_kv_attend) */
   int32_t max_ctx;       /* at least every cached[s] + fresh[s], at most 2^30 */
   int32_t reserved;
@@ -603,7 +604,7 @@ typedef struct {
  * entry is kept.  Writes starts (exclusive sums of fresh), slots and
  * positions (-1 and 0 behind the last token) and status.
  * The step is all or nothing.  When a length is negative, a sequence would
- * pass max_blocks, the tokens pass max_tokens, an id lies outside
+ * pass max_blocks or 2^31 - 1 tokens, the tokens pass max_tokens, an id lies outside
  * [-1, num_blocks), or a block that takes new tokens is named by another
  * entry too (a shared block: copy it first), status[0] is ATP_EINVAL; when
  * too few blocks are free, ATP_ECAPACITY.  block_table then equals `table`,

@@ -3,6 +3,7 @@
 // HIP call; then the launchers of kvstep.hip and attend.hip.
 #include "kvops.h"
 
+#include <algorithm>
 #include <cmath>
 #include <string>
 
@@ -205,6 +206,7 @@ void kv_append(const atp_kv_cache *cache, const atp_kv_step *step, int32_t layer
   AppendArgs a{};
   a.c = check_arena(*cache, layer);
   want(step->max_tokens >= 0, "step: negative size");
+  want(step->max_tokens < (1 << 26), "step: max_tokens must be below 2^26");  // HIP counts a launch's threads in 32 bits
   a.n_q = h.n_q;
   a.dtype = cache->dtype;
   a.cache_dtype = cache->cache_dtype;
@@ -307,7 +309,7 @@ void kv_attend(const atp_kv_cache *cache, const atp_kv_step *step, int32_t layer
   a.cached = step->cached;
   a.scale = mask->scale;
   a.softcap = mask->softcap;
-  a.window = mask->window;
+  a.window = std::min(mask->window, 1 << 30);  // no context is longer, and differences with it stay in 32 bits
   a.slopes = mask->slopes;
   a.q = q;
   a.out = out;

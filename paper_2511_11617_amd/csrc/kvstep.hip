@@ -73,7 +73,7 @@ __device__ inline void new_range(const ExtendArgs &a, int32_t s, int32_t *b, int
 
 __device__ inline bool lengths_fit(const ExtendArgs &a, int32_t s) {
   const int64_t c = a.cached[s], f = a.fresh[s];
-  return c >= 0 && f >= 0 && c + f <= int64_t(a.max_blocks) * a.bt;
+  return c >= 0 && f >= 0 && c + f <= min(int64_t(a.max_blocks) * a.bt, int64_t(INT32_MAX));
 }
 
 __device__ inline uint32_t free_bits(const ExtendArgs &a, const uint32_t *used, int32_t word) {

@@ -212,7 +212,7 @@ def test_attend(name):
 
 MASKS = {
     "softcap": dict(softcap=5.0), "softcap_small": dict(softcap=0.25, scale=3.0), "window_1": dict(window=1),
-    "window_33": dict(window=33), "window_large": dict(window=100000), "slopes": dict(slopes=True),
+    "window_33": dict(window=33), "window_large": dict(window=100000), "window_largest": dict(window=2 ** 31 - 1), "slopes": dict(slopes=True),
     "all": dict(softcap=20.0, window=70, slopes=True, scale=0.3), "scale_0": dict(scale=0.0), "scale_negative": dict(scale=-0.2),
     "sharp": dict(scale=8.0),
 }
@@ -485,6 +485,14 @@ def test_extend_refuses_whole_steps(case):
         cached[1], fresh[1] = 2 ** 31 - 1, 2 ** 31 - 1
     got = check_extend(table, cached, fresh, 4, 9, rows)
     assert got[4] == [atp.EINVAL, 0, 0, 0]
+
+
+def test_extend_refuses_positions_past_31_bits():
+    """A table wide enough for more than 2^31 - 1 tokens of a sequence (blocks of 2^26)."""
+    table = [[-1] * 40]
+    assert run_extend(table, [2 ** 31 - 2], [1], 1 << 26, 50, 1)[4][:2] == [0, 1]
+    got = run_extend(table, [2 ** 31 - 2], [2], 1 << 26, 50, 2)
+    assert got[4] == [atp.EINVAL, 0, 0, 0] and got[2] == [-1, -1] and np.array_equal(got[0], np.asarray(table))
 
 
 def test_extend_keeps_shared_prefixes():

@@ -194,6 +194,10 @@ def test_row_refusals():
     _refused(atp.EALIGN, "lse", _attend, lse=_addr(14) + 2)
 
 
+def test_append_refuses_more_rows_than_a_launch_takes():
+    _refused(atp.EINVAL, "2^26", _append, s=_step(max_tokens=1 << 26))
+
+
 def test_attend_mask_and_bound_refusals():
     _refused(atp.EINVAL, "scale", _attend, mask=atp.Mask(math.nan))
     for cap in (-1.0, 1e-7, math.inf, math.nan):
