@@ -123,6 +123,27 @@ __device__ inline uint32_t finite_only(uint32_t x) {
   if ((x & e << 16) == e << 16) x &= 0xffffu;
   return x;
 }
+// The bytes of four e4m3 values that are NaN (0x7f, 0xff), as their highest bits.
+__device__ inline uint32_t nan_bytes(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+// Whether a row of V (hd elements, a multiple of 8) holds an infinity or NaN.
+template <typename T, typename CT>
+__device__ inline bool not_finite_row(const char *row, int32_t hd) {
+  bool found = false;
+#pragma unroll 4
+  for (int32_t d = 0; d < hd; d += 8) {
+    if constexpr (sizeof(CT) == 2) {
+      const u32x4_t x = *reinterpret_cast<const u32x4_t *>(row + 2 * d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) found |= not_finite<T>(x[j]);
+    } else {
+      const u32x2_t x = *reinterpret_cast<const u32x2_t *>(row + d);
+      found |= (nan_bytes(x[0]) | nan_bytes(x[1])) != 0;
+    }
+  }
+  return found;
+}
+
 // The context's chunks begin at multiples of these.
 constexpr int kFewAlign = 64, kTileAlign = 64;
 constexpr int kFewLeast = 256;  // tokens of the shortest chunk of few rows

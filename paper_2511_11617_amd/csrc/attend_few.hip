@@ -89,7 +89,7 @@ __device__ inline bool clean_word(uint32_t &x) {
     x = y;
     return found;
   } else {
-    const uint32_t nan = ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // bytes of 0x7f or 0xff
+    const uint32_t nan = nan_bytes(x);
     x &= ~((nan >> 7) * 0xffu);
     return nan != 0;
   }
@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
   };
   const bool quads = a.c.bt % 4 == 0;  // 4 tokens from a multiple of 4 on lie in one block
   const int32_t row_step = a.c.tok_stride;
-  int32_t left_lo = INT32_MAX, left_hi = 0;  // the wave's steps with infinities or NaN still to be added
+  int32_t left_lo = INT32_MAX, left_hi = 0;  // the wave's steps with infinities or NaN to be looked for again
   bool bad = false;
   auto block_of = [&](int32_t t) __attribute__((always_inline)) -> int32_t {  // t's block id, -1 for none
     if (t >= hi) return -1;
@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
                        (a.window <= 0 || t0 > q.ctx - 1 - a.window);
     if (!whole) {
       // 0 times an unseen infinity or NaN would be NaN: they become 0 here, and
-      // what of them is seen is added behind the last step
+      // what of them is seen is put in behind the last step
       bool found = false;
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -461,26 +461,63 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
       t0 = t2;
     }
   }
-#pragma unroll 1
-  for (int32_t t1 = left_lo; t1 < left_hi; t1 += kFewWaves * TS)
-#pragma unroll 1
-    for (int32_t t = t1; t < min(t1 + TS, hi); ++t) {
-      const int32_t p = block_of(t);
-      if (p < 0) continue;
-      const CT *const v = reinterpret_cast<const CT *>(vbase + p * a.c.block_stride + int64_t(t - int32_t(divided(t, a.bt_magic)) * a.c.bt) * a.c.tok_stride);
+  // A seen infinity or NaN of V makes its dimension one, whatever its weight:
+  // those cleaned out of a step are still to be added, and in a step that all
+  // rows saw the two parts of a weight (0, or of unlike signs) may have made an
+  // infinity a NaN.  Where such a step left a result that is not finite, the
+  // wave's steps are gone through again (rarely; a score of NaN makes the whole
+  // row one and needs nothing).
+  bool odd = false;
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        if (t > pos[m] || (a.window > 0 && pos[m] - t >= a.window)) continue;
+  for (int m = 0; m < MT; ++m) {
+    sum[m] += __shfl_xor(sum[m], 16);
+    sum[m] += __shfl_xor(sum[m], 32);
+    const bool row_ok = fabsf(sum[m]) <= FLT_MAX;
+#pragma unroll
+    for (int e = 0; e < ND; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) odd |= row_ok & !(fabsf(o[m][e][i]) <= FLT_MAX);
+  }
+  if (__ballot(odd)) {
+    left_lo = lo + wave * TS;
+    left_hi = hi;
+  }
+  if (left_lo < left_hi) {
+    f32x4 wild[MT][ND];  // the sums of what is seen and not finite
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int e = 0; e < ND; ++e) wild[m][e] = f32x4{0, 0, 0, 0};
+#pragma unroll 1
+    for (int32_t t1 = left_lo; t1 < left_hi; t1 += kFewWaves * TS) {
+      const int32_t mine = lane < TS ? block_of(t1 + lane) : -1;  // a token a lane
+      uint64_t which = __ballot(mine >= 0 && not_finite_row<T, CT>(vbase + offset_of(t1 + lane, mine), hd));
+#pragma unroll 1
+      for (; which; which &= which - 1) {
+        const int32_t t = t1 + __builtin_ctzll(which);
+        const CT *const v = reinterpret_cast<const CT *>(vbase + offset_of(t, block_of(t)));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int e = 0; e < ND; ++e) {
             const int d = (4 * grp + i) * ND + e;
             const float y = LIE == WHOLE || d < hd ? as_f32(v[d]) : 0.0f;
-            o[m][e][i] += fabsf(y) <= FLT_MAX ? 0.0f : y;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              const bool sees = t <= pos[m] && (a.window <= 0 || pos[m] - t < a.window);
+              if (sees && !(fabsf(y) <= FLT_MAX)) wild[m][e][i] += y;
+            }
           }
       }
     }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int e = 0; e < ND; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (wild[m][e][i] != 0) o[m][e][i] = wild[m][e][i];  // NaN is not 0 either
+  }
   if (__ballot(bad) && lane == 0) flag(a.status, ATP_EINVAL);
 
   // join the four waves through shared memory, then write the rows
@@ -490,12 +527,9 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
   for (int m = 0; m < MT; ++m) {
     if (m * 16 >= rows) break;
     if (m) __syncthreads();
-    float l = sum[m];
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
     if (grp == 0) {
       stop[wave][col] = top[m];
-      ssum[wave][col] = l;
+      ssum[wave][col] = sum[m];
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
