@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = f32x16{};
 
-  int32_t left_lo = INT32_MAX, left_hi = 0;  // tokens whose infinities and NaN are still to be added
+  int32_t left_lo = INT32_MAX, left_hi = 0;  // tokens whose infinities and NaN are to be looked for again
   bool bad = false;
   auto block_of = [&](int32_t t) -> int32_t {
     if (t >= hi) return -1;
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
 
   // 0 times an unseen infinity or NaN would be NaN: in a tile with something
   // unseen, V's values that are not finite become 0, and what of them is seen
-  // is added behind the last tile.
+  // is put in behind the last tile.
   auto clean = [&](int buf) __attribute__((always_inline)) {
     constexpr int kMine = kTileTokens * ROW / 16 / kTileThreads;
     u32x4_t x[kMine];
@@ -325,28 +325,56 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
       if (more) store(buf ^ 1, g);
     }
   }
-  // A seen infinity or NaN (its weight does not matter) makes its dimension
-  // one; those of a tile that all rows saw are in already, and stay the same.
+  // A seen infinity or NaN of V makes its dimension one, whatever its weight:
+  // those cleaned out of a tile are still to be added, and in a tile that all
+  // rows saw a weight (or a later scale) of 0 may have made one a NaN.  Where
+  // such a tile left a result that is not finite, all tiles are gone through
+  // again (rarely; a score of NaN makes the whole row one and needs nothing).
+  sum += __shfl_xor(sum, 32);
+  bool odd = false;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[d][i]) <= FLT_MAX);
+  if (__ballot(odd & mine & (fabsf(sum) <= FLT_MAX))) {
+    left_lo = lo;
+    left_hi = hi;
+  }
+  if (left_lo < left_hi) {
+    f32x16 wild[DT];  // the sums of what is seen and not finite
+#pragma unroll
+    for (int d = 0; d < DT; ++d) wild[d] = f32x16{};
+    const char *const vbase = kbase + a.c.v_off;
 #pragma unroll 1
-  for (int32_t t = left_lo; t < left_hi; ++t) {
-    const int32_t p = block_of(t);
-    if (p < 0 || t > pos || (a.window > 0 && pos - t >= a.window)) continue;
-    const CT *const v = reinterpret_cast<const CT *>(kbase + a.c.v_off + offset_of(t, p));
+    for (int32_t t0 = left_lo; t0 < left_hi; t0 += kTileTokens) {
+      const int32_t p = block_of(t0 + lane);  // a token a lane
+      uint64_t which = __ballot(p >= 0 && not_finite_row<T, CT>(vbase + offset_of(t0 + lane, p), hd));
+#pragma unroll 1
+      for (; which; which &= which - 1) {
+        const int32_t t = t0 + __builtin_ctzll(which);
+        if (t > pos || (a.window > 0 && pos - t >= a.window)) continue;
+        const CT *const v = reinterpret_cast<const CT *>(vbase + offset_of(t, block_of(t)));
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const int at = 32 * d + 2 * i + 4 * half;
+            if (!WHOLE && at >= hd) continue;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float x = as_f32(v[at + j]);
+              wild[d][i + j] += fabsf(x) <= FLT_MAX ? 0.0f : x;
+            }
+          }
+      }
+    }
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const int at = 32 * d + 2 * i + 4 * half;
-        if (!WHOLE && at >= hd) continue;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float x = as_f32(v[at + j]);
-          o[d][i + j] += fabsf(x) <= FLT_MAX ? 0.0f : x;
-        }
-      }
+      for (int i = 0; i < 16; ++i)
+        if (wild[d][i] != 0) o[d][i] = wild[d][i];  // NaN is not 0 either
   }
   if (__ballot(bad) && lane == 0) flag(a.status, ATP_EINVAL);
-  sum += __shfl_xor(sum, 32);
   if (!mine) return;
   const float inv = sum == 0 ? 0.0f : vs / sum;
   const float lse2 = sum == 0 ? -INFINITY : top + __builtin_amdgcn_logf(sum);

@@ -28,12 +28,18 @@ SHAPES = {
     "dim_256": dict(cached=[700], fresh=[1], hd=256),
     "drafts": dict(cached=[2000], fresh=[4]),
     "long_chunk": dict(cached=[6000] * 64, fresh=[1] * 64),         # several steps a wave
+    "prompt": dict(cached=[0], fresh=[300]),
+    "prompt_cut": dict(cached=[2000], fresh=[40]),                  # tiles in parts, joined
+    "prompt_64_token_major": dict(cached=[600], fresh=[90], hd=64, layout="token"),
+    "prompt_80": dict(cached=[600], fresh=[70], hd=80),
+    "prompt_256": dict(cached=[600], fresh=[70], hd=256),
 }
-CASES = [(n, t, c) for n in SHAPES for t in ("bf16", "fp16") for c in ("same", "e4m3")]
+CASES = [(n, t, c, x) for n in SHAPES for t in ("bf16", "fp16") for c in ("same", "e4m3") for x in ("usual", "sharp")
+         if x == "usual" or n == "prompt"]
 
 
-@pytest.mark.parametrize("scale", ["usual"])
-@pytest.mark.parametrize("name,dtype,cache", CASES)
+# "sharp": scores spread over hundreds, so most weights are 0 in 32 bits, whole chunks' among them
+@pytest.mark.parametrize("name,dtype,cache,scale", CASES)
 def test_attend_non_finite_values_that_are_seen(name, dtype, cache, scale):
     s = Setup(**SHAPES[name], **GQA, dtype=dtype, cache=cache, seed=21)
     ctx, q = s.cached[0] + s.fresh[0], 0
@@ -71,7 +77,7 @@ def test_attend_non_finite_values_that_are_seen(name, dtype, cache, scale):
     assert s.status.tolist()[0] == 0
 
 
-@pytest.mark.parametrize("shape", ["split"])
+@pytest.mark.parametrize("shape", ["split", "prompt_cut"])
 def test_attend_non_finite_values_before_a_window(shape):
     """The same with a window: rows whose window has passed the value keep it out."""
     s = Setup(**SHAPES[shape], **GQA, seed=22)
