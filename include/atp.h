@@ -667,7 +667,8 @@ typedef struct {
  * (out must not overlap q); lse (NULL, or float [max_tokens][query heads])
  * receives the natural logarithm of the sum of exp(score).  A row that sees
  * nothing gives 0 and -infinity.  Values in unseen places, NaN among them, do
- * not matter.  Scores, softmax and sums are held in 32 bits; with many rows
+ * not matter; an infinity or NaN of V that a row sees makes its dimension one,
+ * however small its weight.  Scores, softmax and sums are held in 32 bits; with many rows
  * per KV head the softmax weights enter the second product rounded to dtype.
  * A block id outside [-1, num_blocks) sets status and counts as -1.  A
  * sequence whose starts, cached or lengths break a bound (max_tokens,

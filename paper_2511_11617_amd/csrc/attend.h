@@ -2,6 +2,8 @@
 // operands, a sequence's range of tokens, the score's extras and mask, and
 // the places of tokens in the paged cache.
 #pragma once
+#include <cfloat>
+
 #include "kvdev.h"
 
 namespace atp {
@@ -142,6 +144,12 @@ __device__ inline bool not_finite_row(const char *row, int32_t hd) {
     }
   }
   return found;
+}
+
+// A part's result by its share of the whole; one that is not finite stays so even by 0.
+__device__ inline float shared(float x, float share) { return fabsf(x) <= FLT_MAX ? x * share : x; }
+__device__ inline f32x4 shared(f32x4 x, float share) {
+  return f32x4{shared(x[0], share), shared(x[1], share), shared(x[2], share), shared(x[3], share)};
 }
 
 // The context's chunks begin at multiples of these.

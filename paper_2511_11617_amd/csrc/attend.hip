@@ -9,7 +9,8 @@ namespace atp {
 namespace {
 
 // Joins a row's chunks: out = sum 2^(lse_c - max) out_c / sum 2^(lse_c - max),
-// each chunk's out_c being its own weighted mean, in a fixed order.
+// each chunk's out_c being its own weighted mean, in a fixed order.  An infinity
+// or NaN of V that a chunk's rows saw stays one whatever the chunk's weight.
 
 // Few rows: one workgroup per row and head; 16, 32 or 64 lanes hold its
 // dimensions, 4 each, and as many groups of lanes take chunks in turn.
@@ -65,10 +66,10 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(AttendKernel a, int32_t l
         const int c = c0 + j * groups;
         w[j] = c < chunks ? weight[c] : 0.0f;
         y[j] = f32x4{0, 0, 0, 0};
-        if (w[j] != 0) y[j] = *reinterpret_cast<const f32x4 *>(part + c * step * hd);  // of 0: nothing may have been written
+        if (c < chunks) y[j] = *reinterpret_cast<const f32x4 *>(part + c * step * hd);
       }
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) x += w[j] * y[j];
+      for (int j = 0; j < kAhead; ++j) x += shared(y[j], w[j]);
     }
   }
   acc[tid] = x;
@@ -117,7 +118,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_tiles(AttendKernel a, int
       for (int j = 0; j < kAhead; ++j) {
         const float v = __builtin_amdgcn_exp2f(w[j] - base);
         total += v;
-        o += v * y[j];
+        o += shared(y[j], v);
       }
     }
     const float inv = total == 0 ? 0.0f : 1.0f / total;

@@ -22,8 +22,6 @@
 // Measured: 128 sessions of 8192 tokens, 2 KV heads of 128 in 16 bits, 190 us
 // in this kernel = 5.6 TB/s, where a plain sum over 4 GiB reads 6.1; 3 sessions
 // of up to 131000 in 8 bits, 31 us = 4.9 TB/s.
-#include <cfloat>
-
 #include "attend.h"
 
 namespace atp {
@@ -557,7 +555,7 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
         if (LIE != WHOLE && d >= hd) break;
         f32x4 x = {0, 0, 0, 0};
 #pragma unroll
-        for (int w = 0; w < kFewWaves; ++w) x += *reinterpret_cast<const f32x4 *>(&so[w][r][d]) * f[w];
+        for (int w = 0; w < kFewWaves; ++w) x += shared(*reinterpret_cast<const f32x4 *>(&so[w][r][d]), f[w]);
         x *= inv;
         if (sh.count > 1) {
           *reinterpret_cast<f32x4 *>(a.split.part + (int64_t(blockIdx.x) * a.split.n_split + m * 16 + r) * hd + d) = x;

@@ -23,8 +23,6 @@
 // product of 8192^3 reaches 1270.  A lone wave of a SIMD unit takes 4200 clocks
 // a tile, two together 2700 each, of which the matrix units need 1024: two
 // workgroups a CU, so that one's softmax runs beside the other's products.
-#include <cfloat>
-
 #include "attend.h"
 
 namespace atp {
