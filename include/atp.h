@@ -552,8 +552,10 @@ int atp_kv_evict_lru(const int32_t *table, int32_t n_seq, int32_t max_blocks, in
  * returns; none allocates, waits or copies to the host, so all of them may
  * be captured into a HIP graph.  Workspaces need no initial value and hold
  * nothing from one call to the next; calls that may run at once need
- * workspaces of their own.  Lengths are read on the device: the host gives
- * only bounds (max_*), so a captured step replays with other lengths. */
+ * workspaces of their own.  What a call writes must not overlap anything else
+ * that it reads or writes, but where its text allows it (ATP_EINVAL).
+ * Lengths are read on the device: the host gives only bounds (max_*), so a
+ * captured step replays with other lengths. */
 enum { ATP_BF16 = 0, ATP_FP16 = 1, ATP_E4M3 = 2 }; /* E4M3: OCP, 448 max, NaN, no infinity */
 
 /* The cache of one rank, as the operators see it: the arena of atp_kv with

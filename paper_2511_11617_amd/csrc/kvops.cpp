@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <string>
 
 #include "plan.h"
@@ -44,6 +45,20 @@ Rows rows_of(const void *p, int64_t stride, int64_t heads, int32_t hd, int32_t r
   if (stride >= (int64_t(1) << 40)) bad(ATP_EINVAL, w + ": stride too large");
   if (at(p) % 16 || stride % 8) bad(ATP_EALIGN, w + ": rows must be 16-byte aligned");
   return {at(p), uint64_t(stride) * 2, uint64_t(heads * hd) * 2, uint64_t(rows)};
+}
+
+// A buffer of the call, by its name in a refusal.
+struct Buffer {
+  const char *name;
+  uintptr_t p;
+  uint64_t n;
+};
+
+// Nothing that the kernels write may lie on what they read.
+void check_apart(std::initializer_list<Buffer> written, std::initializer_list<Buffer> read) {
+  for (const Buffer &w : written)
+    for (const Buffer &r : read)
+      if (meet(w.p, w.n, r.p, r.n)) bad(ATP_EINVAL, std::string(w.name) + " overlaps " + r.name);
 }
 
 int elem_bytes(int32_t t) { return t == ATP_E4M3 ? 1 : 2; }
@@ -110,6 +125,13 @@ CacheView check_arena(const atp_kv_cache &c, int32_t layer) {
   return v;
 }
 
+// The arena as far as the cache fills it.
+Buffer arena_of(const atp_kv_cache &c, const CacheView &v) {
+  return {"the arena", at(c.arena), uint64_t(v.v_off) * 2 * uint64_t(c.num_layers)};
+}
+Buffer scales_of(const atp_kv_cache &c) {
+  return {"scales", at(c.scales), c.scales ? uint64_t(c.num_layers) * 2 * uint64_t(n_kv(c)) * 4 : 0};
+}
 
 void check_workspace(const void *ws, uint64_t have, uint64_t need) {
   if (have < need) bad(ATP_ECAPACITY, "workspace too small: " + std::to_string(need) + " bytes are needed");
@@ -252,6 +274,13 @@ void kv_append(const atp_kv_cache *cache, const atp_kv_step *step, int32_t layer
     in[1] = rows_of(k, k_stride, a.c.n_kv, hd, a.max_tokens, "k");
     in[2] = rows_of(v, v_stride, a.c.n_kv, hd, a.max_tokens, "v");
   }
+  const Buffer arena = arena_of(*cache, a.c), turned{"q_out", out.p, out.bytes()},
+      status{"status", at(step->status), step->status ? 4u : 0u};
+  const Buffer slots{"slots", at(step->slots), uint64_t(a.max_tokens) * 8},
+      positions{"positions", at(step->positions), uint64_t(a.max_tokens) * 4}, scales = scales_of(*cache);
+  check_apart({status}, {slots, positions, scales, turned, arena, Buffer{"q", in[0].p, in[0].bytes()},
+                         Buffer{"k", in[1].p, in[1].bytes()}, Buffer{"v", in[2].p, in[2].bytes()}});
+  check_apart({turned, arena}, {slots, positions, scales});
   for (const Rows &r : in) {
     want((&r == in && r.p == out.p && r.stride == out.stride) || !meet(r, out), "q_out overlaps an input");
     want(!meet(r.p, r.bytes(), at(cache->arena), cache->arena_bytes), "the arena overlaps an input");
@@ -295,6 +324,14 @@ void kv_attend(const atp_kv_cache *cache, const atp_kv_step *step, int32_t layer
   const Rows to = rows_of(out, out_stride, a.h.n_q, cache->head_dim, a.max_tokens, "out");
   const uint64_t ws_need = attend_workspace(a), lse_bytes = lse ? uint64_t(a.max_tokens) * a.h.n_q * 4 : 0;
   check_workspace(workspace, workspace_bytes, ws_need);
+  const Buffer arena = arena_of(*cache, a.c), outs{"out", to.p, to.bytes()}, sums{"lse", at(lse), lse_bytes},
+      work{"workspace", at(workspace), ws_need}, status{"status", at(step->status), step->status ? 4u : 0u};
+  const uint64_t seqs = uint64_t(a.n_seq);
+  const Buffer table{"block_table", at(step->block_table), seqs * uint64_t(a.max_blocks) * 4}, cached{"cached", at(step->cached), seqs * 4},
+      starts{"starts", at(step->starts), seqs * 4 + 4}, slopes{"slopes", at(mask->slopes), mask->slopes ? uint64_t(a.h.n_q) * 4 : 0},
+      scales = scales_of(*cache);
+  check_apart({status}, {table, cached, starts, slopes, scales, outs, sums, work, arena, Buffer{"q", in.p, in.bytes()}});
+  check_apart({outs, sums, work}, {table, cached, starts, slopes, scales});
   want(!meet(in, to), "out overlaps q");
   want(!meet(to.p, to.bytes(), at(cache->arena), cache->arena_bytes), "out overlaps the arena");
   want(!meet(at(lse), lse_bytes, to.p, to.bytes()) && !meet(at(lse), lse_bytes, in.p, in.bytes()) &&

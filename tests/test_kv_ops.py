@@ -243,3 +243,50 @@ def test_nothing_to_do_is_ok_without_a_gpu():
     for kw in (dict(n_seq=0), dict(max_tokens=0), dict(max_fresh=0)):
         _attend(s=_step(**kw))
     _attend(_cache(q_heads=(4, 4), kv_heads=(0, 2)))
+
+
+# ---- buffers that a kernel reads while another argument writes them ------------------
+
+
+@pytest.mark.parametrize("read", ["block_table", "cached", "starts", "slopes", "scales"])
+def test_attend_refuses_outputs_over_what_it_reads(read):
+    at = _addr(20)
+    s = dict(n_seq=1, max_blocks=8192, max_tokens=1, max_fresh=1, max_ctx=131072)  # a workspace is needed
+    s, c, m = _step(**s, **({read: at} if read in ("block_table", "cached", "starts") else {})), _cache(), atp.Mask(0.125)
+    if read == "slopes":
+        m = atp.Mask(0.125, slopes=at)
+    elif read == "scales":
+        c = _cache(cache_dtype=atp.E4M3, scales=at)
+    for kw in (dict(o=at), dict(lse=at), dict(ws=at)):
+        _refused(atp.EINVAL, "overlaps", _attend, c, s, mask=m, **kw)
+    # the last word that the call reads and the first behind it
+    words = {"block_table": 8192, "cached": 1, "starts": 2, "slopes": 5, "scales": 8}[read]
+    s.d.status = at + 4 * (words - 1)
+    _refused(atp.EINVAL, "status overlaps", _attend, c, s, mask=m)
+    s.d.status = at + 4 * words
+    _refused(atp.EINVAL, "workspace overlaps", _attend, c, s, mask=m, ws=_addr(0))  # gets past the status
+
+
+@pytest.mark.parametrize("read", ["slots", "positions", "scales"])
+def test_append_refuses_outputs_over_what_it_reads(read):
+    at = _addr(20)
+    c = _cache(cache_dtype=atp.E4M3, scales=at) if read == "scales" else _cache()
+    s = _step(**({} if read == "scales" else {read: at}))
+    _refused(atp.EINVAL, "overlaps", _append, c, s, o=at)
+    c.d.arena = at  # the cache is written too
+    _refused(atp.EINVAL, "overlaps", _append, c, s)
+    c.d.arena = _addr(0)
+    words = {"slots": 16, "positions": 8, "scales": 8}[read]
+    s.d.status = at + 4 * (words - 1)
+    _refused(atp.EINVAL, "status overlaps", _append, c, s)
+    s.d.status = at + 4 * words
+    _refused(atp.EINVAL, "q_out overlaps the arena", _append, c, s, o=_addr(0) + 256)
+
+
+def test_status_apart_from_the_rows_and_the_cache():
+    for f, kw in ((_append, dict(o=_addr(13))), (_attend, dict(o=_addr(13)))):
+        for at in (_addr(13) + 4, _addr(10) + 4, _addr(0) + 4):
+            _refused(atp.EINVAL, "status overlaps", f, s=_step(status=at), **kw)
+    for at in (_addr(14), _addr(9)):
+        s = _step(n_seq=1, max_blocks=8192, max_tokens=1, max_fresh=1, max_ctx=131072, status=at)
+        _refused(atp.EINVAL, "status overlaps", _attend, s=s)
