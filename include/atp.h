@@ -587,7 +587,7 @@ typedef struct {
   int64_t *slots;        /* device [max_tokens]: block * block_tokens +
                             offset of each token, -1 = padding               */
   int32_t *positions;    /* device [max_tokens]: position in its sequence    */
-  int32_t max_tokens;    /* rows (atp_kv_append: below 2^26)                 */
+  int32_t max_tokens;    /* rows (atp_kv_append: at most 2^26 - 4)           */
   int32_t max_fresh;     /* at least every fresh[s]           (atp_kv_attend) */
   int32_t max_ctx;       /* at least every cached[s] + fresh[s], at most 2^30 */
   int32_t reserved;

@@ -228,7 +228,8 @@ void kv_append(const atp_kv_cache *cache, const atp_kv_step *step, int32_t layer
   AppendArgs a{};
   a.c = check_arena(*cache, layer);
   want(step->max_tokens >= 0, "step: negative size");
-  want(step->max_tokens < (1 << 26), "step: max_tokens must be below 2^26");  // HIP counts a launch's threads in 32 bits
+  // HIP counts a launch's threads in 32 bits: 2^24 - 1 workgroups of 256, 4 rows each
+  want(step->max_tokens <= (1 << 26) - 4, "step: max_tokens must be at most 2^26 - 4");
   a.n_q = h.n_q;
   a.dtype = cache->dtype;
   a.cache_dtype = cache->cache_dtype;

@@ -290,3 +290,10 @@ def test_status_apart_from_the_rows_and_the_cache():
     for at in (_addr(14), _addr(9)):
         s = _step(n_seq=1, max_blocks=8192, max_tokens=1, max_fresh=1, max_ctx=131072, status=at)
         _refused(atp.EINVAL, "status overlaps", _attend, s=s)
+
+
+def test_append_takes_rows_up_to_a_launch_of_32_bits_of_threads():
+    """4 rows a workgroup of 256 threads: 2^24 - 1 workgroups are the most."""
+    for rows in ((1 << 26) - 3, (1 << 26) - 1):
+        _refused(atp.EINVAL, "2^26", _append, s=_step(max_tokens=rows))
+    _refused(atp.EINVAL, "q is NULL", _append, s=_step(max_tokens=(1 << 26) - 4), q=0)  # gets past that check
