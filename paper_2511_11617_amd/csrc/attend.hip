@@ -136,35 +136,48 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_tiles(AttendKernel a, int
 // into the list longest first (32 classes of length), so that the last ones to
 // begin are short.  (One prompt of 8192 behind 8192, 576 tiles: cut to shares of
 // 1/640 535 to 557 us, of 1/1024 554, of 1/512 574, not cut 639; 1222 tiles of ragged
-// prompts: not cut 158, cut to 1/640 172.)
+// prompts: not cut 158, cut to 1/640 172, not cut and in no order of length 212.)
 constexpr int kListThreads = 1024, kListTiles = 4096, kClasses = 32;
 constexpr int32_t kTileParts = 640, kTileLeast = 512;
 __global__ void __launch_bounds__(kListThreads) k_list_tiles(AttendKernel a, bool cut) {
   constexpr int kEach = kListTiles / kListThreads;
   __shared__ int64_t sums[kListThreads / 64];
+  __shared__ int32_t spans[kListThreads / 64];
   __shared__ int32_t count[kClasses], from[kClasses], places, n;
   const int tid = threadIdx.x;
   for (int32_t s = tid; s < a.n_seq; s += kListThreads)
     if (!sequence(a, s).ok) flag(a.status, ATP_EINVAL);
   TileItem t[kEach];
   int64_t total = 0;
+  int32_t longest = 0;
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     const int32_t item = j * kListThreads + tid;
     t[j].s = -1;
     if (item < a.split.tiles) t[j] = tile_of(a, item);
-    if (t[j].s >= 0) total += t[j].hi - t[j].lo;
+    if (t[j].s < 0) continue;
+    total += t[j].hi - t[j].lo;
+    longest = max(longest, t[j].hi - t[j].lo);
   }
-  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
-  if ((tid & 63) == 0) sums[tid >> 6] = total;
+  for (int d = 32; d; d >>= 1) {
+    total += __shfl_xor(total, d);
+    longest = max(longest, __shfl_xor(longest, d));
+  }
+  if ((tid & 63) == 0) {
+    sums[tid >> 6] = total;
+    spans[tid >> 6] = longest;
+  }
   if (tid < kClasses) count[tid] = 0;
   if (tid == 0) places = n = 0;
   __syncthreads();
   total = 0;
-  for (int w = 0; w < kListThreads / 64; ++w) total += sums[w];
+  for (int w = 0; w < kListThreads / 64; ++w) {
+    total += sums[w];
+    longest = max(longest, spans[w]);
+  }
   int32_t most = int32_t(min(max((total + kTileParts - 1) / kTileParts, int64_t(kTileLeast)), int64_t(1) << 30));
   if (!cut) most = 1 << 30;
-  const int32_t scale = cut ? most : int32_t(min(int64_t(a.max_ctx), int64_t(1) << 30));
+  const int32_t scale = min(most, longest);  // of the classes; the host's bounds may be far above it
   int32_t parts[kEach], length[kEach], at[kEach];
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
