@@ -668,15 +668,21 @@ typedef struct {
  * their own k and v already (atp_kv_append).  q and out as in atp_kv_append
  * (out must not overlap q); lse (NULL, or float [max_tokens][query heads])
  * receives the natural logarithm of the sum of exp(score).  A row that sees
- * nothing gives 0 and -infinity.  Values in unseen places, NaN among them, do
- * not matter; an infinity or NaN of V that a row sees makes its dimension one,
- * however small its weight.  Scores, softmax and sums are held in 32 bits; with many rows
- * per KV head the softmax weights enter the second product rounded to dtype.
+ * nothing, or whose every score is -infinity, gives 0 and -infinity.  Values
+ * in unseen places, NaN among them, do not matter; an infinity or NaN of V
+ * that a row sees makes its dimension one, however small its weight.
+ * Scores, softmax and sums are held in 32 bits.  With more than 32 rows
+ * (16 where head_dim is above 128) of max_fresh times the query heads of a KV
+ * head, the softmax weights enter the second product rounded to dtype; with
+ * fewer they keep twice its bits.  In fp16 a weight is off by up to 2^-32 of
+ * the row's largest besides.
  * A block id outside [-1, num_blocks) sets status and counts as -1.  A
  * sequence whose starts, cached or lengths break a bound (max_tokens,
  * max_fresh, max_ctx, max_blocks) sets status and its rows are left as they
- * were; starts that do not ascend may leave other rows so too.  The result of a call depends on its inputs and bounds alone (sums
- * are taken in a fixed order).  Uses block_table, cached, starts, max_* and
+ * were; starts that do not ascend may leave other rows so too.  The result of
+ * a call depends on its inputs and bounds alone (sums are taken in a fixed
+ * order).  A step too large for one launch (n_seq * max_fresh * query heads of
+ * 2^24 and more) is ATP_EINVAL.  Uses block_table, cached, starts, max_* and
  * status; the workspace size depends on the bounds. */
 int atp_kv_attend_workspace(const atp_kv_cache *cache, const atp_kv_step *step, uint64_t *bytes);
 int atp_kv_attend(const atp_kv_cache *cache, const atp_kv_step *step, int32_t layer, const atp_kv_mask *mask,

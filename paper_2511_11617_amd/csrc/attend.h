@@ -17,8 +17,12 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // What depends on the 16-bit type.  The softmax weights are taken as 2^(s - m
-// + kLift) with m at most 8 below the largest score: in fp16 the lift keeps
-// weights of 2^-29 of the largest one normal, and 2^15 does not overflow.
+// + kLift) with m at most 8 below the largest score, so that in fp16 the
+// largest, 2^15, does not overflow.  The lift keeps weights of 2^-21 of the
+// largest normal there (2^-29 where that has risen by 2^8 since m was set); a
+// smaller one is off by the type's least half step, 2^-25 / 2^7 = 2^-32 of the
+// largest: over 131072 tokens, 2^-15 of the result in all at most, a sixteenth
+// of its rounding.
 template <typename T>
 struct Half16;
 template <>

@@ -136,7 +136,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_tiles(AttendKernel a, int
 // into the list longest first (32 classes of length), so that the last ones to
 // begin are short.  (One prompt of 8192 behind 8192, 576 tiles: cut to shares of
 // 1/640 535 to 557 us, of 1/1024 554, of 1/512 574, not cut 639; 1222 tiles of ragged
-// prompts: not cut 158, cut to 1/640 172, not cut and in no order of length 212.)
+// prompts: not cut 158, cut to 1/640 172, not cut and in no order of length 212.
+// At 256 dimensions, where the chip holds 256 tiles, 4096 behind 4096: 1/640 432,
+// 1/256 490, 1/320 460, 1/1024 484.)
 constexpr int kListThreads = 1024, kListTiles = 4096, kClasses = 32;
 constexpr int32_t kTileParts = 640, kTileLeast = 512;
 __global__ void __launch_bounds__(kListThreads) k_list_tiles(AttendKernel a, bool cut) {

@@ -18,11 +18,12 @@
 // and fill the row, the loads go straight to shared memory (the lane picks
 // the chunk that belongs at its place).
 //
-// Measured (128 dimensions, bf16): 880 to 970 TFLOP/s where the chip is full
-// (8 prompts of 8192 behind 8192), 840 for one such prompt, where a library
-// product of 8192^3 reaches 1270.  A lone wave of a SIMD unit takes 4200 clocks
-// a tile, two together 2700 each, of which the matrix units need 1024: two
-// workgroups a CU, so that one's softmax runs beside the other's products.
+// Measured (128 dimensions, bf16): 900 TFLOP/s where the chip is full (8 prompts
+// of 8192 behind 8192; 700 from an 8-bit cache), 860 for one such prompt, where
+// a library product of 8192^3 reaches 1270.  In the latter a SIMD unit ends a
+// wave's tile every 2670 clocks (of 2.2 GHz), 1024 of them in its matrix unit,
+// with 1.65 waves on it on average: two workgroups a CU, so that one's softmax
+// runs beside the other's products (a lone wave takes 4200 clocks a tile).
 #include "attend.h"
 
 namespace atp {
@@ -260,6 +261,10 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
     }
     // below any score but not -infinity, so that -infinity - it stays -infinity
     const float ref = top == -INFINITY ? -3.0e38f : top;
+    // The weights are rounded to 16 bits for the second product, their sum is
+    // not: over many tokens that is an error like the output's own rounding (1.4
+    // times in all).  Two parts, as with few rows, would double the product that
+    // bounds this kernel.
     u32x4_t pw[4];
 #pragma unroll
     for (int e = 0; e < 32; e += 2) {
