@@ -150,10 +150,16 @@ __device__ inline bool not_finite_row(const char *row, int32_t hd) {
   return found;
 }
 
-// A part's result by its share of the whole; one that is not finite stays so even by 0.
-__device__ inline float shared(float x, float share) { return fabsf(x) <= FLT_MAX ? x * share : x; }
-__device__ inline f32x4 shared(f32x4 x, float share) {
-  return f32x4{shared(x[0], share), shared(x[1], share), shared(x[2], share), shared(x[3], share)};
+// Whether all four are finite: 0 times anything else is NaN.
+__device__ inline bool all_finite(f32x4 x) {
+  const f32x4 z = x * 0.0f;
+  return (z[0] + z[1]) + (z[2] + z[3]) == 0;
+}
+
+// Adds a part's result by its share of the whole; one that is not finite stays so even by 0.
+__device__ inline void add_share(f32x4 &sum, f32x4 x, float share) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[i] = fabsf(x[i]) <= FLT_MAX ? __builtin_fmaf(x[i], share, sum[i]) : sum[i] + x[i];
 }
 
 // The context's chunks begin at multiples of these.

@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_join(AttendKernel a, int32_t l
         if (c < chunks) y[j] = *reinterpret_cast<const f32x4 *>(part + c * step * hd);
       }
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) x += shared(y[j], w[j]);
+      for (int j = 0; j < kAhead; ++j) add_share(x, y[j], w[j]);
     }
   }
   acc[tid] = x;
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_tiles(AttendKernel a, int
       for (int j = 0; j < kAhead; ++j) {
         const float v = __builtin_amdgcn_exp2f(w[j] - base);
         total += v;
-        o += shared(y[j], v);
+        add_share(o, y[j], v);
       }
     }
     const float inv = total == 0 ? 0.0f : 1.0f / total;

@@ -470,11 +470,10 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
   for (int m = 0; m < MT; ++m) {
     sum[m] += __shfl_xor(sum[m], 16);
     sum[m] += __shfl_xor(sum[m], 32);
-    const bool row_ok = fabsf(sum[m]) <= FLT_MAX;
+    f32x4 z = {0, 0, 0, 0};  // 0, or NaN
 #pragma unroll
-    for (int e = 0; e < ND; ++e)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) odd |= row_ok & !(fabsf(o[m][e][i]) <= FLT_MAX);
+    for (int e = 0; e < ND; ++e) z += o[m][e] * 0.0f;
+    odd |= fabsf(sum[m]) <= FLT_MAX && !all_finite(z);
   }
   if (__ballot(odd)) {
     left_lo = lo + wave * TS;
@@ -555,7 +554,11 @@ __global__ void __launch_bounds__(kFewWaves * 64, HD == 256 || (HD == 128 && MT 
         if (LIE != WHOLE && d >= hd) break;
         f32x4 x = {0, 0, 0, 0};
 #pragma unroll
-        for (int w = 0; w < kFewWaves; ++w) x += shared(*reinterpret_cast<const f32x4 *>(&so[w][r][d]), f[w]);
+        for (int w = 0; w < kFewWaves; ++w) x += *reinterpret_cast<const f32x4 *>(&so[w][r][d]) * f[w];
+        if (!all_finite(x)) {
+          x = f32x4{0, 0, 0, 0};
+          for (int w = 0; w < kFewWaves; ++w) add_share(x, *reinterpret_cast<const f32x4 *>(&so[w][r][d]), f[w]);
+        }
         x *= inv;
         if (sh.count > 1) {
           *reinterpret_cast<f32x4 *>(a.split.part + (int64_t(blockIdx.x) * a.split.n_split + m * 16 + r) * hd + d) = x;

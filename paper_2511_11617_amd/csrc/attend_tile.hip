@@ -334,12 +334,12 @@ __global__ void __launch_bounds__(kTileThreads, HD == 256 ? 1 : 2) k_tile(Attend
   // such a tile left a result that is not finite, all tiles are gone through
   // again (rarely; a score of NaN makes the whole row one and needs nothing).
   sum += __shfl_xor(sum, 32);
-  bool odd = false;
+  f32x4 z = {0, 0, 0, 0};  // 0, or NaN
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[d][i]) <= FLT_MAX);
-  if (__ballot(odd & mine & (fabsf(sum) <= FLT_MAX))) {
+    for (int i = 0; i < 16; i += 4) z += f32x4{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]} * 0.0f;
+  if (__ballot(mine && fabsf(sum) <= FLT_MAX && !all_finite(z))) {
     left_lo = lo;
     left_hi = hi;
   }
